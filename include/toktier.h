@@ -175,6 +175,87 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
              void* workspace, size_t workspace_bytes);
 
 /*
+ * Scores of token ids: what a model's logits say about the ids that tt_encode* left (the log probability of each, with
+ * the text offsets of tt_spans, is what an API returns beside a completion and what a model is trained on).
+ *
+ * tt_logprobs -- for every row x of n_vocab logits, with z = scale * x and the probabilities p = softmax(z):
+ *   logprob  ln p[t] of the row's id t          entropy  -sum p ln p
+ *   lse      ln sum exp z                       rank     1 + number of entries before t in the order below
+ *   top      the top_k first entries in the order below and their ln p
+ * The order is by logit, the larger first, equal ones (0 and -0 are equal) by index, the lower first.
+ *   logits      DEVICE, n_rows rows of n_vocab entries of `dtype`, row_stride entries apart (>= n_vocab, any alignment that the
+ *               type itself needs).  n_vocab < 2^31, n_rows < 2^24.
+ *   scale       > 0 and finite (1 / temperature).
+ *   ids         DEVICE int32[n_rows].  ids_off = NULL: row i is asked for ids[i]; a negative id asks for nothing.
+ *   ids_off     DEVICE int64[n_docs + 1] as tt_encode_batch leaves it, or NULL (then n_docs is 0): row i is what the model said behind
+ *               token i, and is asked for ids[i + 1] if that token is of the same document, else for nothing.  Rows from
+ *               ids_off[n_docs] on are not read and nothing of theirs is written.
+ *   logprob_out, lse_out, entropy_out  DEVICE float[n_rows]; rank_out DEVICE int32[n_rows]; any but logprob_out may be NULL.
+ *   top_ids_out, top_logprob_out       DEVICE int32 / float [n_rows][top_k], top_k <= TT_TOP_MAX and <= n_vocab; top_k = 0: both NULL.
+ *   status_out  DEVICE int32: TT_OK; TT_ERR_CAPACITY if ids_off[n_docs] > n_rows (nothing else is written); else TT_ERR_ARG if ids_off does not
+ *               ascend from 0 (what is written is then unspecified, but in place); else TT_ERR_BAD_IDS if a row is asked for an id outside
+ *               [0, n_vocab) (without ids_off: of n_vocab or more), and is then treated as asked for nothing.
+ * A row asked for nothing has logprob 0 and rank 0.  Logits of -inf, or so low that their probability is 0 in 32 bits, count as
+ * probability 0.  A row of -inf alone: lse and all ln p are -inf, entropy 0.  A row with a NaN or a +inf: lse, entropy and all ln p are NaN
+ * (the logprob of a row asked for nothing stays 0), rank 0, top ids -1.  Sums are held in 32 bits.  The outputs do not overlap the inputs.
+ *
+ * tt_logprobs_grad -- the gradient: given g = dL/dlogprob and h = dL/dentropy of every row (and lse, entropy as tt_logprobs left them for the
+ * same logits, ids, offsets and scale),   dL/dx[j] = scale * ( g ([j = t] - p[j]) - h p[j] (ln p[j] + entropy) ),   without the g part where the row is
+ * asked for nothing.
+ *   grad_logprob   DEVICE float[n_rows].   grad_entropy, entropy  DEVICE float[n_rows], or both NULL (h = 0).
+ *   grad_out       DEVICE, `dtype`, rows grad_stride entries apart: every row in use is written as a whole (n_vocab entries), the rows
+ *                  behind the last document are left as they were.  It may be `logits` itself with the same stride; other overlaps are not allowed.
+ * A row whose g and h are both 0 (g also where it is asked for nothing) gets zeros, and its logits are not read; so does a row whose lse is -inf.  A row whose lse is
+ * NaN gets NaN.  status_out as above; the rest of the arguments too.
+ * Both are asynchronous on `stream`, allocate nothing, need no workspace and may be captured into a graph.
+ */
+enum { TT_BF16 = 0, TT_FP16 = 1, TT_FP32 = 2 };
+#define TT_TOP_MAX 32
+int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t n_vocab, size_t row_stride, float scale, const int32_t* ids,
+                const int64_t* ids_off, size_t n_docs, size_t top_k, void* stream, float* logprob_out, float* lse_out, float* entropy_out,
+                int32_t* rank_out, int32_t* top_ids_out, float* top_logprob_out, int32_t* status_out);
+int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, size_t n_vocab, size_t row_stride, float scale, const int32_t* ids,
+                     const int64_t* ids_off, size_t n_docs, const float* lse, const float* entropy, const float* grad_logprob,
+                     const float* grad_entropy, void* stream, void* grad_out, size_t grad_stride, int32_t* status_out);
+
+/*
+ * Block tables: where the tokens of tt_encode_batch go in a paged cache, worked out on the device from their offsets.  The cache
+ * consists of blocks of block_size token slots; a request's tokens 0, 1, 2, ... lie in the blocks that its row of the table lists.
+ *   block_table  DEVICE int32[n_req][table_width]: row r lists ceil(seq_len[r] / block_size) blocks; entries behind them mean nothing.
+ *   seq_len      DEVICE int32[n_req]: tokens of each request in the cache.
+ *   free_blocks  DEVICE int32[free_cap], of which the first *n_free (DEVICE int64) are free block ids, taken from and given back at the end.
+ *                Ids are not looked at: what a caller puts there comes back in tables and slots.
+ *
+ * tt_blocks_extend -- requests grow by new_off[r + 1] - new_off[r] tokens each (ids_off of tt_encode_batch, or one token a request in a decode
+ * step; a request may get none).  Blocks are taken for whole requests in order: with k counted through all blocks taken, the k-th is
+ * free_blocks[*n_free - 1 - k].  Token i of the packed batch, of request r, gets
+ *   pos_out[i] = seq_len[r] + i - new_off[r],  slots_out[i] = block_table[r][pos / block_size] * block_size + pos % block_size,  req_out[i] = r.
+ *   new_off      DEVICE int64[n_req + 1], ascending from 0, at most slots_cap.
+ *   slots_out    DEVICE int64[slots_cap]; pos_out, req_out DEVICE int32[slots_cap], either may be NULL.  Entries from new_off[n_req] on
+ *                are left as they were.
+ *   seq_len_out, n_free_out   DEVICE: the new lengths and the new number of free blocks.  Each may be the input's own buffer (a step that is
+ *                captured once and replayed) or another one that does not overlap it.
+ * tt_blocks_release -- requests shrink to keep_len[r] tokens (0: the request is over; the part of a session that an append kept): the blocks behind
+ * ceil(keep_len[r] / block_size) return to the list, in the order that undoes tt_blocks_extend: extending and then releasing to the
+ * lengths before leaves list and count as they were.  The table is not written.
+ *   status_out   DEVICE int32: TT_OK; TT_ERR_ARG: new_off does not ascend from 0, a length is negative, keep_len[r] > seq_len[r], or *n_free
+ *                is outside [0, free_cap]; TT_ERR_CAPACITY: too few free blocks (release: no room in the list), a request too long for table_width
+ *                (or 2^31 - 1 tokens), more tokens than slots_cap.  TT_ERR_ARG comes first.  In either case the table, the list and the maps stay as they
+ *                were, and seq_len_out and n_free_out get the lengths and the number that there were.
+ *   workspace    DEVICE scratch of tt_blocks_workspace_bytes(n_req), 256-byte aligned, for calls that do not overlap in time.
+ * n_req < 2^24, block_size and table_width < 2^31, slots_cap < 2^31, free_cap < 2^31; n_req = 0 gives TT_OK and copies *n_free.  Asynchronous on `stream`,
+ * may be captured into a graph.
+ */
+size_t tt_blocks_workspace_bytes(size_t n_req);
+int tt_blocks_extend(const int64_t* new_off, size_t n_req, const int32_t* seq_len, size_t block_size, int32_t* block_table, size_t table_width,
+                     const int32_t* free_blocks, size_t free_cap, const int64_t* n_free, void* stream, int64_t* slots_out, size_t slots_cap,
+                     int32_t* pos_out, int32_t* req_out, int32_t* seq_len_out, int64_t* n_free_out, int32_t* status_out,
+                     void* workspace, size_t workspace_bytes);
+int tt_blocks_release(const int32_t* keep_len, size_t n_req, const int32_t* seq_len, size_t block_size, const int32_t* block_table, size_t table_width,
+                      int32_t* free_blocks, size_t free_cap, const int64_t* n_free, void* stream, int32_t* seq_len_out, int64_t* n_free_out,
+                      int32_t* status_out, void* workspace, size_t workspace_bytes);
+
+/*
  * Added tokens (paper Sec. 4.3 / 4.4: added and special tokens are literal strings reserved as single ids; a
  * leftmost-longest literal pass extracts them before the tokenizer family handles the remaining segments).
  *   tt_vocab_add_literals  registers n literals once per vocabulary (HOST arrays, copied): literal i is

@@ -18,11 +18,14 @@ TT_OK, TT_ERR_ARG, TT_ERR_BAD_VOCAB, TT_ERR_CUDA, TT_ERR_INVALID_UTF8, TT_ERR_CA
 TT_STATIC_MAX_LEN = 262144
 TT_PATTERN_CL100K, TT_PATTERN_O200K, TT_PATTERN_CL100K_N1, TT_PATTERN_SPLIT3 = 0, 1, 2, 3
 TT_VOCAB_IGNORE_MERGES = 1
+TT_BF16, TT_FP16, TT_FP32 = 0, 1, 2
+TT_TOP_MAX = 32
 
 EXPORTS = ["tt_vocab_load", "tt_vocab_load_ex", "tt_vocab_free", "tt_vocab_table_entries", "tt_workspace_bytes", "tt_encode", "tt_encode_batch",
            "tt_pretokenize", "tt_encode_timed", "tt_encode_host", "tt_encode_static", "tt_spans", "tt_spans_workspace_bytes", "tt_class_table", "tt_strerror",
            "tt_session_create", "tt_session_free", "tt_session_set_window", "tt_session_append", "tt_session_view", "tt_session_copy", "tt_session_tokens", "tt_vocab_add_literals", "tt_encode_added",
-           "tt_pair_info_host", "tt_verifier_create", "tt_verifier_submit", "tt_verifier_drain", "tt_verifier_get_stats", "tt_verifier_quarantined", "tt_verifier_free"]
+           "tt_pair_info_host", "tt_verifier_create", "tt_verifier_submit", "tt_verifier_drain", "tt_verifier_get_stats", "tt_verifier_quarantined", "tt_verifier_free",
+           "tt_logprobs", "tt_logprobs_grad", "tt_blocks_workspace_bytes", "tt_blocks_extend", "tt_blocks_release"]
 
 _lib = None
 REFERENCE_FN = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p, ctypes.c_size_t,
@@ -109,6 +112,20 @@ def lib() -> ctypes.CDLL:
         L.tt_session_tokens.argtypes = [c.c_void_p]
         L.tt_session_copy.restype = c.c_int
         L.tt_session_copy.argtypes = [c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p, c.c_void_p, c.c_void_p]
+        L.tt_logprobs.restype = c.c_int
+        L.tt_logprobs.argtypes = [c.c_void_p, c.c_int, c.c_size_t, c.c_size_t, c.c_size_t, c.c_float, c.c_void_p, c.c_void_p, c.c_size_t, c.c_size_t,
+                                  c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p]
+        L.tt_logprobs_grad.restype = c.c_int
+        L.tt_logprobs_grad.argtypes = [c.c_void_p, c.c_int, c.c_size_t, c.c_size_t, c.c_size_t, c.c_float, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p,
+                                       c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p]
+        L.tt_blocks_workspace_bytes.restype = c.c_size_t
+        L.tt_blocks_workspace_bytes.argtypes = [c.c_size_t]
+        L.tt_blocks_extend.restype = c.c_int
+        L.tt_blocks_extend.argtypes = [c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p,
+                                       c.c_void_p, c.c_void_p, c.c_size_t, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t]
+        L.tt_blocks_release.restype = c.c_int
+        L.tt_blocks_release.argtypes = [c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p, c.c_size_t, c.c_void_p,
+                                        c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t]
         _lib = L
     return _lib
 
@@ -345,6 +362,149 @@ class Session:
                "tt_session_copy")
         torch.cuda.synchronize()
         return ids[:k], off, n.value
+
+
+# -- around the model: scores of ids, block tables -------------------------------------------------------------------
+
+
+def _dev(t, dtype, name, numel=None, device=None):
+    """Device address of a contiguous CUDA tensor of this type (and size, on this device); raises ValueError otherwise."""
+    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} CUDA tensor is needed")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"{name}: {numel} entries are needed, {t.numel()} given")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name}: on {t.device}, other arguments on {device}")
+    return t.data_ptr()
+
+
+def _on(device, stream, call):
+    """call(stream address) with `device` current, on `stream` (a stream of that device) or that device's current stream."""
+    import torch
+    if stream is not None and stream.device != device:
+        raise ValueError(f"stream of {stream.device}, tensors on {device}")
+    if device.index == torch.cuda.current_device():
+        return call(_stream_ptr(stream))
+    with torch.cuda.device(device):
+        return call(_stream_ptr(stream))
+
+
+def _logits(logits, name="logits"):
+    """(type code, rows, entries of a row, distance of rows) of a 2-D CUDA tensor whose entries of a row are neighbours."""
+    import torch
+    kinds = {torch.bfloat16: TT_BF16, torch.float16: TT_FP16, torch.float32: TT_FP32}
+    if logits.dtype not in kinds or not logits.is_cuda or logits.dim() != 2:
+        raise ValueError(f"{name}: a 2-D bfloat16, float16 or float32 CUDA tensor is needed")
+    rows, n = logits.shape
+    step, one = logits.stride()
+    if n > 1 and one != 1:
+        raise ValueError(f"{name}: the entries of a row have to be neighbours")
+    return kinds[logits.dtype], rows, n, max(step, n) if rows <= 1 else step
+
+
+def alloc_logprobs(n_rows: int, top_k: int = 0, device="cuda") -> dict:
+    """Device buffers for logprobs(): dict(logprob, lse, entropy, rank, status and, with top_k, top_ids, top_logprobs), zeroed."""
+    import torch
+    f = dict(dtype=torch.float32, device=device)
+    i = dict(dtype=torch.int32, device=device)
+    out = dict(logprob=torch.zeros(n_rows, **f), lse=torch.zeros(n_rows, **f), entropy=torch.zeros(n_rows, **f),
+               rank=torch.zeros(n_rows, **i), status=torch.zeros(1, **i))
+    if top_k:
+        out.update(top_ids=torch.zeros((n_rows, top_k), **i), top_logprobs=torch.zeros((n_rows, top_k), **f))
+    return out
+
+
+def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None):
+    """tt_logprobs: logits = bfloat16 / float16 / float32 CUDA tensor [n_rows, n_vocab] (rows may lie apart), ids = int32 CUDA tensor
+    [n_rows], ids_off = int64 CUDA tensor [n_docs + 1] (as encode_batch leaves it) or None.  Results land in bufs as alloc_logprobs makes them; 'logprob'
+    and 'status' have to be there, the others are left out where they are missing; the second size of 'top_ids' is top_k."""
+    import torch
+    kind, rows, n, step = _logits(logits)
+    dev = logits.device
+
+    def out(name, dtype, numel=rows):
+        t = bufs.get(name)
+        return None if t is None else _dev(t, dtype, name, numel, dev)
+
+    top = bufs.get("top_ids")
+    if (top is None) != (bufs.get("top_logprobs") is None) or (top is not None and (top.dim() != 2 or top.shape[0] != rows)):
+        raise ValueError("top_ids and top_logprobs: both [n_rows, top_k], or neither")
+    k = 0 if top is None else top.shape[1]
+    args = (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
+            None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1, k)
+    outs = (_dev(bufs["logprob"], torch.float32, "logprob", rows, dev), out("lse", torch.float32), out("entropy", torch.float32),
+            out("rank", torch.int32), out("top_ids", torch.int32, rows * k) if k else None, out("top_logprobs", torch.float32, rows * k) if k else None,
+            _dev(bufs["status"], torch.int32, "status", 1, dev))
+    _check(_on(dev, stream, lambda st: lib().tt_logprobs(*args, st, *outs)), "tt_logprobs")
+
+
+def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entropy=None, scale: float = 1.0, stream=None):
+    """tt_logprobs_grad: bufs as logprobs() left them for the same logits, ids, ids_off and scale ('lse', with grad_entropy also 'entropy';
+    'status' is written again).  grad_logprob / grad_entropy: float32 CUDA tensors [n_rows]; grad: like logits, or logits itself."""
+    import torch
+    kind, rows, n, step = _logits(logits)
+    dev = logits.device
+    gkind, grows, gn, gstep = _logits(grad, "grad")
+    if (gkind, grows, gn) != (kind, rows, n) or grad.device != dev:
+        raise ValueError("grad: of the type, size and device of logits")
+    args = (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
+            None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1,
+            _dev(bufs["lse"], torch.float32, "lse", rows, dev), None if grad_entropy is None else _dev(bufs["entropy"], torch.float32, "entropy", rows, dev),
+            _dev(grad_logprob, torch.float32, "grad_logprob", rows, dev),
+            None if grad_entropy is None else _dev(grad_entropy, torch.float32, "grad_entropy", rows, dev))
+    status = _dev(bufs["status"], torch.int32, "status", 1, dev)
+    _check(_on(dev, stream, lambda st: lib().tt_logprobs_grad(*args, st, grad.data_ptr(), gstep, status)), "tt_logprobs_grad")
+
+
+def alloc_blocks(n_req: int, table_width: int, n_blocks: int, max_tokens: int, device="cuda"):
+    """(state, bufs) for blocks_extend / blocks_release: n_req empty requests, all n_blocks blocks free, maps for up to max_tokens new tokens.
+    bufs['seq_len'] and bufs['n_free'] are the state's own tensors, so that every call moves the state on."""
+    import torch
+    i = dict(dtype=torch.int32, device=device)
+    state = dict(block_table=torch.full((n_req, table_width), -1, **i), seq_len=torch.zeros(n_req, **i),
+                 free_blocks=torch.arange(n_blocks - 1, -1, -1, **i), n_free=torch.full((1,), n_blocks, dtype=torch.int64, device=device))
+    bufs = dict(slots=torch.full((max_tokens,), -1, dtype=torch.int64, device=device), positions=torch.zeros(max_tokens, **i),
+                requests=torch.zeros(max_tokens, **i), seq_len=state["seq_len"], n_free=state["n_free"], status=torch.zeros(1, **i),
+                workspace=torch.empty(int(lib().tt_blocks_workspace_bytes(n_req)), dtype=torch.uint8, device=device))
+    return state, bufs
+
+
+def _blocks(state, bufs, block_size):
+    """The arguments that both calls share: (device, requests, those before the stream, those behind it)."""
+    import torch
+    table, free = state["block_table"], state["free_blocks"]
+    if table.dim() != 2:
+        raise ValueError("block_table: [n_req, table_width] is needed")
+    n, dev = table.shape[0], table.device
+    if block_size <= 0:
+        raise ValueError("block_size: at least 1")
+    ws = bufs["workspace"]
+    before = (_dev(state["seq_len"], torch.int32, "seq_len", n, dev), block_size, _dev(table, torch.int32, "block_table"), table.shape[1],
+              _dev(free, torch.int32, "free_blocks", None, dev), free.numel(), _dev(state["n_free"], torch.int64, "n_free", 1, dev))
+    behind = (_dev(bufs["seq_len"], torch.int32, "seq_len", n, dev), _dev(bufs["n_free"], torch.int64, "n_free", 1, dev),
+              _dev(bufs["status"], torch.int32, "status", 1, dev), _dev(ws, torch.uint8, "workspace", None, dev), ws.numel())
+    return dev, n, before, behind
+
+
+def blocks_extend(new_off, state, block_size: int, bufs, stream=None):
+    """tt_blocks_extend: new_off = int64 CUDA tensor [n_req + 1] (encode_batch's ids_off, or a decode step's).  state: dict(seq_len, block_table,
+    free_blocks, n_free); bufs: dict(slots, seq_len, n_free, status, workspace and, if wanted, positions, requests), see alloc_blocks."""
+    import torch
+    dev, n, before, behind = _blocks(state, bufs, block_size)
+    slots = bufs["slots"]
+    cap = slots.numel()
+    maps = [None if bufs.get(k) is None else _dev(bufs[k], torch.int32, k, cap, dev) for k in ("positions", "requests")]
+    off = _dev(new_off, torch.int64, "new_off", n + 1, dev)
+    sp = _dev(slots, torch.int64, "slots", None, dev)
+    _check(_on(dev, stream, lambda st: lib().tt_blocks_extend(off, n, *before, st, sp, cap, *maps, *behind)), "tt_blocks_extend")
+
+
+def blocks_release(keep_len, state, block_size: int, bufs, stream=None):
+    """tt_blocks_release: keep_len = int32 CUDA tensor [n_req], tokens that each request keeps; state and bufs as for blocks_extend."""
+    import torch
+    dev, n, before, behind = _blocks(state, bufs, block_size)
+    keep = _dev(keep_len, torch.int32, "keep_len", n, dev)
+    _check(_on(dev, stream, lambda st: lib().tt_blocks_release(keep, n, *before, st, *behind)), "tt_blocks_release")
 
 
 class VerifierStats(ctypes.Structure):

@@ -5,7 +5,7 @@ import subprocess
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libtoktier.so")
-SOURCES = [os.path.join(CSRC, "toktier.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("toktier.cu", "tt_scores.cu", "tt_blocks.cu")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-shared", "-Xcompiler", "-fPIC"]
 

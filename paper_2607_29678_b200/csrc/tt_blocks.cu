@@ -1,0 +1,52 @@
+// C ABI of the block tables (see include/toktier.h): tt_blocks_extend and tt_blocks_release.  Nothing here synchronises or allocates.
+#include "../../include/toktier.h"
+#include "tt_blocks.cuh"
+
+static size_t blocks_up(size_t x) { return (x + 255) / 256 * 256; }
+
+extern "C" size_t tt_blocks_workspace_bytes(size_t n_req) { return blocks_up(sizeof(BlocksPlan)) + blocks_up(n_req * sizeof(int2)); }
+
+static int blocks_args(BlocksParams& P, size_t n_req, const int32_t* seq_len, size_t block_size, const int32_t* table, size_t width, const int32_t* free_blocks,
+                       size_t free_cap, const int64_t* n_free, int32_t* seq_out, int64_t* n_free_out, int32_t* status_out, void* workspace, size_t workspace_bytes) {
+    const size_t most = (size_t)1 << 31;
+    if (n_req >= ((size_t)1 << 24) || !block_size || block_size >= most || width >= most || free_cap >= most) return TT_ERR_ARG;
+    if (!n_free || !n_free_out || !status_out || !workspace || (n_req && (!seq_len || !seq_out || (width && !table))) || (free_cap && !free_blocks)) return TT_ERR_ARG;
+    if (((uintptr_t)workspace & 255) != 0 || workspace_bytes < tt_blocks_workspace_bytes(n_req)) return TT_ERR_ARG;
+    P = BlocksParams{};
+    P.seq_len = seq_len; P.n_req = (u32)n_req; P.block = (u32)block_size; P.width = (u32)width; P.table = const_cast<int32_t*>(table);
+    P.free_blocks = const_cast<int32_t*>(free_blocks); P.free_cap = free_cap; P.n_free = (const long long*)n_free;
+    P.seq_out = seq_out; P.n_free_out = (long long*)n_free_out; P.status_out = status_out;
+    P.plan = (BlocksPlan*)workspace; P.per = (int2*)((char*)workspace + blocks_up(sizeof(BlocksPlan)));
+    return TT_OK;
+}
+
+extern "C" int tt_blocks_extend(const int64_t* new_off, size_t n_req, const int32_t* seq_len, size_t block_size, int32_t* block_table, size_t table_width,
+                                const int32_t* free_blocks, size_t free_cap, const int64_t* n_free, void* stream, int64_t* slots_out, size_t slots_cap,
+                                int32_t* pos_out, int32_t* req_out, int32_t* seq_len_out, int64_t* n_free_out, int32_t* status_out,
+                                void* workspace, size_t workspace_bytes) {
+    BlocksParams P;
+    const int rc = blocks_args(P, n_req, seq_len, block_size, block_table, table_width, free_blocks, free_cap, n_free, seq_len_out, n_free_out, status_out, workspace, workspace_bytes);
+    if (rc != TT_OK) return rc;
+    if ((n_req && !new_off) || slots_cap >= ((size_t)1 << 31) || (slots_cap && !slots_out)) return TT_ERR_ARG;
+    P.new_off = (const long long*)new_off; P.slots = (long long*)slots_out; P.slots_cap = slots_cap; P.pos = pos_out; P.req = req_out;
+    const int sms = host_sm_count();
+    if (!sms) return TT_ERR_CUDA;
+    TT_TRY(host_launch(k_blocks_plan<true>, 1, BLOCKS_THREADS, 1, 0, (cudaStream_t)stream, P));
+    if (n_req) TT_TRY(host_launch(k_blocks_extend, (unsigned)sms * 8, 256, 1, 0, (cudaStream_t)stream, P));
+    return TT_OK;
+}
+
+extern "C" int tt_blocks_release(const int32_t* keep_len, size_t n_req, const int32_t* seq_len, size_t block_size, const int32_t* block_table, size_t table_width,
+                                 int32_t* free_blocks, size_t free_cap, const int64_t* n_free, void* stream, int32_t* seq_len_out, int64_t* n_free_out,
+                                 int32_t* status_out, void* workspace, size_t workspace_bytes) {
+    BlocksParams P;
+    const int rc = blocks_args(P, n_req, seq_len, block_size, block_table, table_width, free_blocks, free_cap, n_free, seq_len_out, n_free_out, status_out, workspace, workspace_bytes);
+    if (rc != TT_OK) return rc;
+    if (n_req && !keep_len) return TT_ERR_ARG;
+    P.keep = keep_len;
+    const int sms = host_sm_count();
+    if (!sms) return TT_ERR_CUDA;
+    TT_TRY(host_launch(k_blocks_plan<false>, 1, BLOCKS_THREADS, 1, 0, (cudaStream_t)stream, P));
+    if (n_req) TT_TRY(host_launch(k_blocks_release, (unsigned)sms * 8, 256, 1, 0, (cudaStream_t)stream, P));
+    return TT_OK;
+}

@@ -1,0 +1,37 @@
+// What the entry points that need no vocabulary (scores of ids, block tables) share: types, error returns, launches, the device's size.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+#include <cuda_runtime.h>
+
+typedef uint32_t u32;
+typedef uint64_t u64;
+
+#define TT_TRY(x) do { if ((x) != cudaSuccess) { cudaGetLastError(); return TT_ERR_CUDA; } } while (0)
+
+// SMs of the current device, 0 on an error (asked for at every call: an attribute query costs well under a microsecond, and the
+// current device may change between calls).
+static inline int host_sm_count() {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) { cudaGetLastError(); return 0; }
+    return n;
+}
+
+// Launches `kernel` in clusters of `cluster` CTAs (1: none) so that it may be placed while the kernel before it on the stream drains; every
+// CTA waits inside (cudaGridDependencySynchronize) before it touches memory that kernel may write.
+template <typename... KernelParams, typename... Params>
+static cudaError_t host_launch(void (*kernel)(KernelParams...), unsigned grid, unsigned block, unsigned cluster, size_t smem, cudaStream_t st, const Params&... p) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    cfg.attrs = attr;
+    return cudaLaunchKernelEx(&cfg, kernel, p...);
+}

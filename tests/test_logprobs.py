@@ -1,0 +1,542 @@
+"""Scores of token ids (tt_logprobs, tt_logprobs_grad) against their definition in 64 bits, and their refusals.
+
+Tolerances, with e = 2^-24 (half a step of 32 bits), d_j = scale (x_j - max), E the mean under the row's probabilities:
+each exp d_j is off by at most 2^-22 (the hardware's exponential) + 3 e |d_j| (three roundings on the way to its exponent) relative to itself, a
+sum that one of at least 128 threads takes over its share of the row and that is then joined by at most 32 more additions adds e (n / 128 + 32):
+  S = 2^-22 + e (3 E|d| + n / 128 + 32)                            relative error of sum exp d, so the absolute one of its logarithm
+  logprob: S + e (3 |d_t| + 2 ln s)      lse: S + 3 e |scale max| + 2 e (ln s + |lse|)
+  entropy: S + 2 e ln s + E|d| (S + 2^-22 + e (n / 128 + 36)) + 3 e E d^2 + 2 e entropy
+"""
+import ctypes
+
+import numpy as np
+import pytest
+
+EPS = 2.0 ** -24
+KINDS = ["bf16", "fp16", "fp32"]
+
+
+@pytest.fixture(scope="module")
+def tt():
+    from paper_2607_29678_b200 import build
+    build.build()
+    import paper_2607_29678_b200 as m
+    return m
+
+
+def _kind(name):
+    import torch
+    return {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[name]
+
+
+# ---- the definition in 64 bits ------------------------------------------------------------------------------------
+
+
+def targets(ids, ids_off, n_vocab):
+    """Per row: the id asked for, -1 for none, -2 for a row that is not in use."""
+    ids = np.asarray(ids, dtype=np.int64)
+    if ids_off is None:
+        return np.where((ids >= 0) & (ids < n_vocab), ids, -1)
+    t = np.full(ids.size, -2, dtype=np.int64)
+    for a, b in zip(ids_off[:-1], ids_off[1:]):
+        for i in range(a, b):
+            nxt = ids[i + 1] if i + 1 < b else -1
+            t[i] = nxt if 0 <= nxt < n_vocab else -1
+    return t
+
+
+def order(x):
+    """The entries of a row, the larger first, equal ones by index."""
+    return np.lexsort((np.arange(x.size), -(x + 0.0)))
+
+
+def row_scores(x, scale, t, k):
+    """dict of one row's outputs and their tolerances; x in 64 bits."""
+    n = x.size
+    if np.isnan(x).any() or (x == np.inf).any():
+        return dict(logprob=0.0 if t < 0 else np.nan, lse=np.nan, entropy=np.nan, rank=0, top_ids=np.full(k, -1), top_logprobs=np.full(k, np.nan), tol={})
+    at = order(x)
+    place = np.empty(n, dtype=np.int64)
+    place[at] = np.arange(n)
+    rank = 0 if t < 0 else int(place[t]) + 1
+    m = x.max()
+    if m == -np.inf:
+        return dict(logprob=0.0 if t < 0 else -np.inf, lse=-np.inf, entropy=0.0, rank=rank, top_ids=at[:k], top_logprobs=np.full(k, -np.inf), tol={})
+    d = scale * (x - m)
+    p = np.exp(d)
+    s = p.sum()
+    p /= s
+    ls = np.log(s)
+    low = p > 0
+    e_d, e_dd = -(p[low] * d[low]).sum(), (p[low] * d[low] ** 2).sum()
+    ent = ls + e_d
+    S = 2.0 ** -22 + EPS * (3 * e_d + n / 128 + 32)
+    lse = scale * m + ls
+    lp_tol = lambda v: S + EPS * (3 * np.abs(v) + 2 * ls)  # noqa: E731
+    finite = lambda v: np.where(np.isfinite(v), v, 0.0)  # noqa: E731
+    return dict(logprob=0.0 if t < 0 else d[t] - ls, lse=lse, entropy=ent, rank=rank, top_ids=at[:k], top_logprobs=d[at[:k]] - ls,
+                tol=dict(logprob=lp_tol(finite(d[t])) if t >= 0 else 0.0, lse=S + 3 * EPS * abs(scale * m) + 2 * EPS * (ls + abs(lse)),
+                         entropy=S + 2 * EPS * ls + e_d * (S + 2.0 ** -22 + EPS * (n / 128 + 36)) + 3 * EPS * e_dd + 2 * EPS * ent, top_logprobs=lp_tol(finite(d[at[:k]]))))
+
+
+def near(got, want, tol):
+    got, want = np.asarray(got, dtype=np.float64), np.asarray(want, dtype=np.float64)
+    plain = np.isfinite(want)
+    # a log probability below what 32 bits hold (masks of the type's lowest value) may come back as -inf
+    far = plain & (want < -3.0e38)
+    same = np.where(far, got < -3.0e38, np.where(plain, np.abs(got - np.where(plain, want, 0.0)) <= tol, (got == want) | (np.isnan(got) & np.isnan(want))))
+    return bool(np.all(same))
+
+
+def check_scores(logits, ids, bufs, ids_off=None, scale=1.0, untouched=None):
+    """Every row of bufs against the definition; rows not in use hold what `untouched` holds."""
+    x = logits.double().cpu().numpy()
+    t = targets(ids.cpu().numpy(), None if ids_off is None else ids_off.cpu().numpy(), x.shape[1])
+    got = {k: v.cpu().numpy() for k, v in bufs.items()}
+    k = got["top_ids"].shape[1] if "top_ids" in got else 0
+    scale = float(np.float32(scale))
+    for i in range(x.shape[0]):
+        if t[i] == -2:
+            for name in got:
+                if name != "status":
+                    assert np.array_equal(got[name][i], untouched[name][i], equal_nan=True), (i, name)
+            continue
+        w = row_scores(x[i], scale, t[i], k)
+        for name in ("logprob", "lse", "entropy", "top_logprobs"):
+            if name in got:
+                assert near(got[name][i], w[name], w["tol"].get(name, 0.0)), (i, name, got[name][i], w[name], w["tol"].get(name))
+        if "rank" in got:
+            assert got["rank"][i] == w["rank"], (i, got["rank"][i], w["rank"])
+        if k:
+            assert np.array_equal(got["top_ids"][i], w["top_ids"]), (i, got["top_ids"][i], w["top_ids"])
+
+
+def row_grad(x, scale, t, lse, ent, g, h):
+    """(gradient, tolerance before the rounding to the output's type) of one row from its definition; lse and ent as handed to the kernel."""
+    g = g if t >= 0 else 0.0
+    if (g == 0 and h == 0) or lse == -np.inf:
+        return np.zeros_like(x), np.zeros_like(x)
+    lp = scale * x - lse
+    p = np.exp(lp)
+    lpz = np.where(p > 0, lp, 0.0)
+    hot = np.zeros_like(x)
+    if t >= 0:
+        hot[t] = 1.0
+    dx = scale * (g * (hot - p) - h * p * (lpz + ent))
+    rel = 2.0 ** -22 + 4 * EPS * np.abs(lpz) + 4 * EPS                   # of p: the exponent's roundings and the hardware's exponential
+    tol = scale * ((abs(g) + abs(h) * np.abs(lpz + ent)) * p * (rel + 6 * EPS) + 4 * EPS * abs(g) * hot + 3 * EPS * abs(h) * p * (np.abs(lpz) + abs(ent)))
+    return dx, tol + 2.0 ** -120                                           # (what is below the normal numbers of 32 bits may be 0)
+
+
+def check_grad(logits, ids, bufs, g, h, grad, ids_off=None, scale=1.0, untouched=None):
+    import torch
+    x = logits.double().cpu().numpy()
+    t = targets(ids.cpu().numpy(), None if ids_off is None else ids_off.cpu().numpy(), x.shape[1])
+    lse, ent = bufs["lse"].double().cpu().numpy(), bufs["entropy"].double().cpu().numpy()
+    got = grad.double().cpu().numpy()
+    half = torch.finfo(grad.dtype).eps / 2
+    least = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 0.0}[grad.dtype]     # half the smallest subnormal
+    scale = float(np.float32(scale))
+    for i in range(x.shape[0]):
+        if t[i] == -2:
+            assert np.array_equal(got[i], untouched[i]), i
+            continue
+        hi = 0.0 if h is None else float(h[i])
+        want, tol = row_grad(x[i], scale, t[i], lse[i], ent[i], float(g[i]), hi)
+        if np.isnan(lse[i]) and not (hi == 0 and (float(g[i]) == 0 or t[i] < 0)):
+            assert np.isnan(got[i]).all(), i
+            continue
+        off = np.abs(got[i] - want) - (tol + half * (np.abs(want) + tol) + least)
+        assert off.max() <= 0, (i, int(off.argmax()), got[i][off.argmax()], want[off.argmax()], tol[off.argmax()])
+
+
+# ---- on the CPU: the definition itself, refusals -------------------------------------------------------------------
+
+
+def test_definition_on_hand_examples():
+    w = row_scores(np.log(np.array([1.0, 2.0, 4.0, 1.0])), 1.0, 3, 4)
+    assert np.isclose(w["logprob"], np.log(1 / 8)) and np.isclose(w["lse"], np.log(8)) and w["rank"] == 4
+    assert np.isclose(w["entropy"], -(2 / 8 * np.log(1 / 8) + 2 / 8 * np.log(2 / 8) + 4 / 8 * np.log(4 / 8)))
+    assert list(w["top_ids"]) == [2, 1, 0, 3]
+    assert list(targets([5, 6, 7, 8, 9], [0, 2, 2, 4], 8)) == [6, -1, -1, -1, -2]
+    assert list(targets([5, -1, 9], None, 8)) == [5, -1, -1]
+
+
+def test_definition_gradient_against_differences():
+    rng = np.random.default_rng(0)
+    x, step = rng.normal(0, 2, 9), 1e-5
+    for scale, g, h, t in ((1.0, 1.0, 0.0, 4), (0.7, -0.5, 0.3, 0), (1.3, 0.0, 1.0, -1)):
+        loss = lambda y: (lambda w: (g * w["logprob"] if t >= 0 else 0.0) + h * w["entropy"])(row_scores(y, scale, t, 0))  # noqa: E731
+        w = row_scores(x, scale, t, 0)
+        dx, _ = row_grad(x, scale, t, w["lse"], w["entropy"], g, h)
+        num = np.array([(loss(x + step * np.eye(9)[j]) - loss(x - step * np.eye(9)[j])) / (2 * step) for j in range(9)])
+        assert np.abs(num - dx).max() < 1e-8
+
+
+def test_refusals_without_a_device(tt):
+    """Arguments are looked at before any CUDA call: the addresses here are never used."""
+    L, a = tt.lib(), 0x1000
+
+    def fwd(logits=a, dtype=0, rows=2, n=8, stride=8, scale=1.0, ids=a, off=None, docs=0, k=0, lp=a, top_i=None, top_l=None, status=a):
+        return L.tt_logprobs(logits, dtype, rows, n, stride, scale, ids, off, docs, k, None, lp, None, None, None, top_i, top_l, status)
+
+    bad = [dict(logits=None), dict(logits=a + 1), dict(logits=a + 2, dtype=2), dict(dtype=3), dict(dtype=-1), dict(n=0), dict(n=1 << 31, stride=1 << 31), dict(rows=1 << 24),
+           dict(stride=7), dict(stride=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(ids=None), dict(docs=1),
+           dict(lp=None), dict(status=None), dict(k=9, top_i=a, top_l=a), dict(k=33, n=64, stride=64, top_i=a, top_l=a), dict(k=1), dict(k=1, top_i=a), dict(top_i=a, top_l=a),
+           dict(off=a, docs=1 << 31)]
+    for kw in bad:
+        assert fwd(**kw) == tt.TT_ERR_ARG, kw
+
+    def bwd(logits=a, rows=2, n=8, stride=8, lse=a, ent=None, g=a, h=None, grad=2 * a, gstride=8, status=a, dtype=0):
+        return L.tt_logprobs_grad(logits, dtype, rows, n, stride, 1.0, a, None, 0, lse, ent, g, h, None, grad, gstride, status)
+
+    for kw in [dict(lse=None), dict(g=None), dict(h=a), dict(ent=a), dict(grad=None), dict(gstride=7), dict(grad=a, gstride=9), dict(grad=2 * a + 1), dict(status=None), dict(dtype=5)]:
+        assert bwd(**kw) == tt.TT_ERR_ARG, kw
+
+
+def test_binding_refuses_what_does_not_fit(tt):
+    import torch
+    x = torch.zeros((2, 8))
+    bufs = tt.alloc_logprobs(2, device="cpu")
+    with pytest.raises(ValueError):
+        tt.logprobs(x, torch.zeros(2, dtype=torch.int32), bufs)             # not on a device
+    with pytest.raises(ValueError):
+        tt.logprobs(x.double(), torch.zeros(2, dtype=torch.int32), bufs)
+
+
+# ---- on the GPU ----------------------------------------------------------------------------------------------------
+
+
+def make_logits(kind, rows, n, seed, pad=0, shift=0, spread=2.5):
+    """Random logits as a view whose rows lie n + pad entries apart, `shift` entries behind an aligned address."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    step = n + pad
+    whole = torch.full((rows * step + shift,), 77.0, dtype=_kind(kind), device="cuda")
+    x = whole[shift:].view(rows, step)[:, :n]
+    x.copy_(torch.randn((rows, n), generator=g, device="cuda") * spread)
+    return x
+
+
+def make_ids(rows, n, seed, none_every=0):
+    import torch
+    g = torch.Generator().manual_seed(seed + 1)
+    ids = torch.randint(0, n, (rows,), generator=g, dtype=torch.int32)
+    if none_every:
+        ids[::none_every] = -1
+    return ids.cuda()
+
+
+def run_scores(tt, x, ids, k=0, ids_off=None, scale=1.0, fill=None, status=0):
+    import torch
+    bufs = tt.alloc_logprobs(x.shape[0], k)
+    for name, v in bufs.items():
+        v.fill_(-7)
+    before = {name: v.cpu().numpy().copy() for name, v in bufs.items()}
+    tt.logprobs(x, ids, bufs, ids_off=ids_off, scale=scale)
+    torch.cuda.synchronize()
+    assert int(bufs["status"].item()) == status
+    return bufs, before
+
+
+SHAPES = [(1, 1, 0), (1, 1, 1), (3, 2, 2), (2, 7, 5), (5, 31, 31), (4, 33, 32), (3, 255, 4), (2, 1_000, 32), (2, 4_352, 5), (7, 4_353, 20), (2, 32_257, 32), (1, 100_256, 5),
+          (150, 5_003, 3), (300, 2_048, 1), (2, 200_001, 20)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,n,k", SHAPES)
+@pytest.mark.parametrize("kind", KINDS)
+def test_scores_match_the_definition(tt, kind, rows, n, k):
+    for pad, shift, scale in ((0, 0, 1.0), (3, 1, 0.7)):
+        x = make_logits(kind, rows, n, seed=rows * n + k + pad, pad=pad, shift=shift)
+        ids = make_ids(rows, n, n + pad, none_every=4 if rows > 3 else 0)
+        bufs, _ = run_scores(tt, x, ids, k, scale=scale)
+        check_scores(x, ids, bufs, scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 5, 129, 3_001, 20_000, 65_537])
+def test_scores_of_masked_and_broken_rows(tt, kind, n):
+    """Masks of -inf and of the type's lowest value, rows with nothing left, rows of one value, signed zeros, NaN and +inf."""
+    import torch
+    low, inf = torch.finfo(_kind(kind)).min, float("inf")
+    x = make_logits(kind, 16, n, seed=n)
+    gone = torch.rand((16, n), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") < 0.9
+    x[0].masked_fill_(gone[0], -inf)
+    x[1].masked_fill_(gone[1], low)
+    x[2] = -inf
+    x[3] = low
+    x[4] = low; x[4].masked_fill_(gone[4], -inf)                           # the lowest value is all there is, beside -inf
+    x[5] = 0.0; x[5, ::2] = -0.0
+    x[6] = 3.0
+    x[7, n // 2] = float("nan")
+    x[8, n // 3] = inf
+    x[9] = float("nan")
+    x[10] = -inf; x[10, n - 1] = -4.0                                      # one entry left
+    x[11] = -inf; x[11, n // 2] = float("nan")
+    x[12] = torch.finfo(_kind(kind)).max
+    x[13] = low; x[13, n // 2] = torch.finfo(_kind(kind)).max              # a distance of twice the largest value
+    x[14] = inf
+    x[15] = inf; x[15, 0] = -inf
+    ids = make_ids(16, n, n)
+    ids[10] = n - 1
+    for scale in (1.0, 1.5):
+        bufs, _ = run_scores(tt, x, ids, min(n, 32), scale=scale)
+        if scale != 1.0 and kind != "fp16":                                # scale * max passes 32 bits: the lse is an infinity
+            assert bufs["lse"][12].item() == inf and bufs["lse"][3].item() == -inf
+            del bufs["lse"]
+        check_scores(x, ids, bufs, scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [257, 8_200, 50_001, 150_000])
+def test_alternatives_where_the_largest_lie_together(tt, kind, n):
+    """Sorted rows, plateaus of equal values, large values at regular distances: whatever the shares that threads take of a row."""
+    import torch
+    rows = []
+    j = torch.arange(n, device="cuda")
+    rows.append(-j.float() / n)
+    rows.append(j.float() / n)
+    rows.append((j // 40).float() / 64)
+    rows.append((n - 1 - j).float() // 100)
+    for step in (2, 8, 64, 512, 1_024, 2_048, 4_096, 8_192, 16_384):
+        rows.append(torch.where(j % step == step // 2, 5.0 + (j % 1_000).float() / 128, torch.zeros((), device="cuda")))
+        rows.append(torch.where((j % (8 * step)) // 8 == 1, 5.0 + (j // 8 % 61).float() / 64, torch.zeros((), device="cuda")))
+    x = torch.stack(rows).to(_kind(kind))
+    ids = make_ids(len(rows), n, n)
+    for k in (1, 7, 32):
+        bufs, _ = run_scores(tt, x, ids, k)
+        check_scores(x, ids, bufs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,off", [(12, [0, 5, 12]), (12, [0, 0, 1, 1, 9, 9]), (7, [0, 0]), (9, [0, 1, 2, 3, 4]), (5, [0]), (200, list(range(0, 191, 3)) + [190]), (70, [0] * 40 + [70])])
+def test_packed_documents(tt, kind, rows, off):
+    """Row i scores token i + 1 of its own document; the rows behind the last one keep what they held, gradients too."""
+    import torch
+    n = 515
+    x = make_logits(kind, rows, n, seed=rows)
+    ids = make_ids(rows, n, rows)
+    toff = torch.tensor(off, dtype=torch.int64, device="cuda")
+    bufs, before = run_scores(tt, x, ids, 3, ids_off=toff)
+    check_scores(x, ids, bufs, ids_off=toff, untouched=before)
+    g = torch.randn(rows, device="cuda")
+    g[::5] = 0.0
+    h = torch.randn(rows, device="cuda")
+    h[::2] = 0.0
+    for hh in (None, h):
+        grad = torch.full_like(x, 9.0)
+        tt.logprobs_grad(x, ids, bufs, g, grad, ids_off=toff, grad_entropy=hh)
+        torch.cuda.synchronize()
+        assert int(bufs["status"].item()) == 0
+        check_grad(x, ids, bufs, g, hh, grad, ids_off=toff, untouched=np.full((rows, n), 9.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,n", [(1, 1), (2, 2), (3, 7), (2, 129), (5, 4_352), (7, 4_353), (2, 32_257), (40, 1_000), (1, 200_001)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradient_matches_the_definition(tt, kind, rows, n):
+    import torch
+    for pad, shift, gpad, scale in ((0, 0, 0, 1.0), (3, 1, 5, 0.7), (5, 1, 5, 1.5)):
+        x = make_logits(kind, rows, n, seed=rows * n + pad, pad=pad, shift=shift)
+        ids = make_ids(rows, n, n + pad, none_every=4 if rows > 3 else 0)
+        bufs, _ = run_scores(tt, x, ids, scale=scale)
+        g, h = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+        for hh in (None, h):
+            whole = torch.full((rows, n + gpad), 5.0, dtype=x.dtype, device="cuda")
+            grad = whole[:, :n]
+            tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=hh, scale=scale)
+            torch.cuda.synchronize()
+            assert int(bufs["status"].item()) == 0
+            check_grad(x, ids, bufs, g, hh, grad, scale=scale)
+            assert bool((whole[:, n:] == 5.0).all())
+        same = x.clone() if pad == 0 else x
+        want = grad.clone()
+        tt.logprobs_grad(same, ids, bufs, g, same, grad_entropy=h, scale=scale)          # in place of the logits
+        assert torch.equal(same, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradient_of_masked_and_broken_rows(tt, kind):
+    import torch
+    n, inf, low = 1_003, float("inf"), torch.finfo(_kind(kind)).min
+    x = make_logits(kind, 8, n, seed=3)
+    gone = torch.rand((8, n), generator=torch.Generator(device="cuda").manual_seed(5), device="cuda") < 0.9
+    x[0].masked_fill_(gone[0], -inf)
+    x[1].masked_fill_(gone[1], low)
+    x[2] = -inf
+    x[3] = low if kind == "fp16" else -5.0
+    x[4, 17] = float("nan")
+    x[5, 17] = inf
+    x[6, 17] = float("nan")
+    x[7] = -inf; x[7, 5] = 1.0
+    ids = make_ids(8, n, 1)
+    bufs, _ = run_scores(tt, x, ids)
+    g, h = torch.randn(8, device="cuda"), torch.randn(8, device="cuda")
+    g[6] = h[6] = 0.0                                                      # nothing is asked of the broken row: zeros
+    grad = torch.full_like(x, 5.0)
+    tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=h)
+    check_grad(x, ids, bufs, g, h, grad)
+    assert bool((grad[2] == 0).all()) and bool((grad[6] == 0).all()) and bool(torch.isnan(grad[4:6].float()).all())
+    assert bool((grad[0][gone[0]] == 0).sum() >= gone[0].sum() - 1)
+
+
+@pytest.mark.gpu
+def test_gradient_against_differences_of_the_definition(tt):
+    """Central differences of the scores in 64 bits, step 1e-5: off by some 1e-9 themselves."""
+    import torch
+    x = make_logits("fp32", 3, 40, seed=9)
+    ids = make_ids(3, 40, 2)
+    bufs, _ = run_scores(tt, x, ids, scale=1.25)
+    g, h = torch.tensor([1.0, -0.5, 0.25], device="cuda"), torch.tensor([0.5, 1.0, -2.0], device="cuda")
+    grad = torch.zeros_like(x)
+    tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=h, scale=1.25)
+    xs, step = x.double().cpu().numpy(), 1e-5
+    for i in range(3):
+        t = int(ids[i])
+        f = lambda y: float(g[i]) * row_scores(y, 1.25, t, 0)["logprob"] + float(h[i]) * row_scores(y, 1.25, t, 0)["entropy"]  # noqa: E731
+        num = np.array([(f(xs[i] + step * np.eye(40)[j]) - f(xs[i] - step * np.eye(40)[j])) / (2 * step) for j in range(40)])
+        lse, ent = float(bufs["lse"][i]), float(bufs["entropy"][i])
+        _, tol = row_grad(xs[i], 1.25, t, lse, ent, float(g[i]), float(h[i]))
+        # the lse and entropy handed over are off by at most their own tolerance: p by that much relative to itself
+        w = row_scores(xs[i], 1.25, t, 0)["tol"]
+        p = np.exp(1.25 * xs[i] - lse)
+        more = 1.25 * p * (w["lse"] * (abs(float(g[i])) + abs(float(h[i])) * (np.abs(np.log(p) + ent) + 1)) + abs(float(h[i])) * w["entropy"])
+        assert (np.abs(grad[i].double().cpu().numpy() - num) <= tol + more + 1e-8 + EPS * np.abs(num)).all()
+
+
+@pytest.mark.gpu
+def test_statuses(tt):
+    import torch
+    n = 100
+    x = make_logits("bf16", 10, n, seed=1)
+    ids = make_ids(10, n, 1)
+    off = lambda *v: torch.tensor(v, dtype=torch.int64, device="cuda")  # noqa: E731
+    wrong = ids.clone(); wrong[4] = n
+    bufs, before = run_scores(tt, x, wrong, status=tt.TT_ERR_BAD_IDS)
+    check_scores(x, wrong, bufs)                                           # that row counts as asked for nothing
+    assert bufs["logprob"][4].item() == 0 and bufs["rank"][4].item() == 0
+    run_scores(tt, x, wrong, ids_off=off(0, 4, 10))                        # the first token of a document is asked for by no row
+    run_scores(tt, x, wrong, ids_off=off(0, 4))                            # nor is one behind the documents
+    run_scores(tt, x, wrong, ids_off=off(0, 4, 4, 4, 10))
+    run_scores(tt, x, wrong, ids_off=off(0, 3, 10), status=tt.TT_ERR_BAD_IDS)
+    wrong[4] = -1
+    run_scores(tt, x, wrong)
+    run_scores(tt, x, wrong, ids_off=off(0, 10), status=tt.TT_ERR_BAD_IDS)
+    run_scores(tt, x, ids, ids_off=off(0, 6, 5), status=tt.TT_ERR_ARG)
+    run_scores(tt, x, ids, ids_off=off(1, 6, 8), status=tt.TT_ERR_ARG)
+    run_scores(tt, x, ids, ids_off=off(0, -1), status=tt.TT_ERR_ARG)
+    bufs, before = run_scores(tt, x, ids, 2, ids_off=off(0, 11), status=tt.TT_ERR_CAPACITY)
+    for name in bufs:
+        assert name == "status" or np.array_equal(bufs[name].cpu().numpy(), before[name])
+    grad = torch.full_like(x, 5.0)
+    tt.logprobs_grad(x, ids, bufs, torch.ones(10, device="cuda"), grad, ids_off=off(0, 11))
+    torch.cuda.synchronize()
+    assert int(bufs["status"].item()) == tt.TT_ERR_CAPACITY and bool((grad == 5.0).all())
+    # no rows at all
+    empty = tt.alloc_logprobs(0)
+    empty["status"].fill_(-7)
+    tt.logprobs(x[:0], ids[:0], empty)
+    assert int(empty["status"].item()) == 0
+
+
+@pytest.mark.gpu
+def test_outputs_that_are_not_wanted(tt):
+    import torch
+    x = make_logits("fp16", 5, 777, seed=1)
+    ids = make_ids(5, 777, 1)
+    full, _ = run_scores(tt, x, ids, 4)
+    for names in (["logprob"], ["logprob", "rank"], ["logprob", "entropy", "top_ids", "top_logprobs"], ["logprob", "lse"]):
+        bufs = {k: torch.zeros_like(full[k]) for k in names + ["status"]}
+        tt.logprobs(x, ids, bufs)
+        for k in names:
+            assert torch.equal(bufs[k], full[k]), k
+
+
+@pytest.mark.gpu
+def test_rows_beyond_32_bit_offsets(tt):
+    """The last rows lie more than 2^32 bytes (and 2^31 entries) behind the first."""
+    import torch
+    rows, step, n = 1_030, 1 << 21, 301
+    whole = torch.empty((rows, step), dtype=torch.bfloat16, device="cuda")
+    x = whole[:, :n]
+    x.copy_(torch.randn((rows, n), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda"))
+    ids = make_ids(rows, n, 1)
+    bufs, _ = run_scores(tt, x, ids, 2)
+    check_scores(x[-8:], ids[-8:], {k: v[-8:] if k != "status" else v for k, v in bufs.items()})
+    g = torch.randn(rows, device="cuda")
+    want = torch.zeros((rows, n), dtype=torch.bfloat16, device="cuda")
+    tt.logprobs_grad(x, ids, bufs, g, want)
+    check_grad(x[-8:], ids[-8:], {k: v[-8:] for k, v in bufs.items() if k != "status"}, g[-8:], None, want[-8:])
+    tt.logprobs_grad(x, ids, bufs, g, x)
+    assert torch.equal(x, want)
+
+
+@pytest.mark.gpu
+def test_streams_capture_and_repetition(tt):
+    """On another stream, captured and replayed on new contents, two graphs side by side; the same inputs give the same bits."""
+    import torch
+    x, y = make_logits("bf16", 33, 32_257, seed=1), make_logits("bf16", 33, 32_257, seed=2)
+    ids = make_ids(33, 32_257, 1)
+    want, _ = run_scores(tt, x, ids, 20)
+    g = torch.randn(33, device="cuda")
+    dx = torch.zeros_like(x)
+    tt.logprobs_grad(x, ids, want, g, dx)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    live = x.clone()
+    graphs = []
+    for _ in range(2):
+        bufs = tt.alloc_logprobs(33, 20)
+        grad = torch.zeros_like(x)
+        with torch.cuda.stream(side):
+            tt.logprobs(live, ids, bufs, stream=side)
+            tt.logprobs_grad(live, ids, bufs, g, grad)
+        side.synchronize()
+        assert torch.equal(grad, dx)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            tt.logprobs(live, ids, bufs)
+            tt.logprobs_grad(live, ids, bufs, g, grad)
+        graphs.append((graph, bufs, grad))
+    live.copy_(y)
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for (graph, _, _), st in zip(graphs, (side, other)):
+        with torch.cuda.stream(st):
+            graph.replay()
+    torch.cuda.synchronize()
+    ref, _ = run_scores(tt, y, ids, 20)
+    for _, bufs, grad in graphs:
+        for k in ref:
+            assert torch.equal(bufs[k], ref[k]), k
+        again = torch.zeros_like(grad)
+        tt.logprobs_grad(y, ids, ref, g, again)
+        assert torch.equal(grad, again)
+    live.copy_(x)
+    graphs[0][0].replay()
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(graphs[0][1][k], want[k]), k
+
+
+@pytest.mark.gpu
+def test_binding_refuses_on_a_device(tt):
+    import torch
+    x = make_logits("bf16", 4, 50, seed=1)
+    ids = make_ids(4, 50, 1)
+    bufs = tt.alloc_logprobs(4, 2)
+    for bad in (lambda: tt.logprobs(x, ids.long(), bufs), lambda: tt.logprobs(x, ids[:3], bufs), lambda: tt.logprobs(x.t(), ids, bufs), lambda: tt.logprobs(x[0], ids, bufs),
+                lambda: tt.logprobs(x, ids, {**bufs, "top_ids": bufs["top_ids"][:, :1]}), lambda: tt.logprobs(x, ids, {k: v for k, v in bufs.items() if k != "top_logprobs"}),
+                lambda: tt.logprobs(x, ids, {**bufs, "lse": bufs["lse"].double()}), lambda: tt.logprobs(x, ids, bufs, ids_off=torch.zeros(2, dtype=torch.int32, device="cuda")),
+                lambda: tt.logprobs_grad(x, ids, bufs, bufs["lse"], x.float()), lambda: tt.logprobs_grad(x, ids, bufs, bufs["lse"][:2], x)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(tt.TokTierError):
+        tt.logprobs(x[:1].expand(4, 50), ids, bufs)                        # rows that lie over one another
+    with pytest.raises(tt.TokTierError):
+        tt.logprobs(x, ids, bufs, scale=0.0)
