@@ -185,7 +185,7 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
  * The order is by logit, the larger first, equal ones (0 and -0 are equal) by index, the lower first.
  *   logits      DEVICE, n_rows rows of n_vocab entries of `dtype`, row_stride entries apart (>= n_vocab, any alignment that the
  *               type itself needs).  n_vocab < 2^31, n_rows < 2^24.
- *   scale       > 0 and finite (1 / temperature).
+ *   scale       > 0 and at most 2^100 (1 / temperature).
  *   ids         DEVICE int32[n_rows].  ids_off = NULL: row i is asked for ids[i]; a negative id asks for nothing.
  *   ids_off     DEVICE int64[n_docs + 1] as tt_encode_batch leaves it, or NULL (then n_docs is 0): row i is what the model said behind
  *               token i, and is asked for ids[i + 1] if that token is of the same document, else for nothing.  Rows from

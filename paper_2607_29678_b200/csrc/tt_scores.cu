@@ -2,8 +2,6 @@
 #include "../../include/toktier.h"
 #include "tt_scores.cuh"
 
-#include <cmath>
-
 static size_t score_size(int dtype) { return dtype == TT_FP32 ? 4 : 2; }
 
 // What both entry points check of their arguments.
@@ -12,8 +10,14 @@ static int score_args(const void* logits, int dtype, size_t n_rows, size_t n_voc
     if (dtype != TT_BF16 && dtype != TT_FP16 && dtype != TT_FP32) return TT_ERR_ARG;
     if (!status_out || (n_rows && (!logits || !ids)) || !n_vocab || n_vocab >= ((size_t)1 << 31) || n_rows >= ((size_t)1 << 24)) return TT_ERR_ARG;
     if (row_stride < n_vocab || row_stride >= ((size_t)1 << 38) || ((uintptr_t)logits & (score_size(dtype) - 1)) != 0) return TT_ERR_ARG;
-    if (!(scale > 0.0f) || !std::isfinite(scale) || (ids_off == nullptr && n_docs != 0) || n_docs >= ((size_t)1 << 31)) return TT_ERR_ARG;
+    if (!(scale > 0.0f && scale <= 0x1p100f) || (ids_off == nullptr && n_docs != 0) || n_docs >= ((size_t)1 << 31)) return TT_ERR_ARG;
     return TT_OK;
+}
+
+template <typename T>
+static cudaError_t launch_logprobs(const ScoreParams& P, unsigned ctas, cudaStream_t st) {
+    const auto kernel = P.top_k ? (P.rank ? k_logprobs<T, true, true> : k_logprobs<T, true, false>) : P.rank ? k_logprobs<T, false, true> : k_logprobs<T, false, false>;
+    return host_launch(kernel, ((unsigned)P.n_rows + 1) * ctas, SCORE_NT, ctas, 0, st, P);
 }
 
 extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t n_vocab, size_t row_stride, float scale, const int32_t* ids,
@@ -28,8 +32,14 @@ extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t 
     P.ids = ids; P.ids_off = (const long long*)ids_off; P.n_docs = n_docs;
     P.logprob = logprob_out; P.lse = lse_out; P.entropy = entropy_out; P.rank = rank_out; P.top_ids = top_ids_out; P.top_lp = top_logprob_out;
     P.status_out = status_out;
-    const auto kernel = dtype == TT_BF16 ? k_logprobs<__nv_bfloat16> : dtype == TT_FP16 ? k_logprobs<__half> : k_logprobs<float>;
-    TT_TRY(host_launch(kernel, (unsigned)n_rows + 1, SCORE_THREADS, 1, 0, (cudaStream_t)stream, P));
+    P.scale2 = (float)((double)scale * 1.4426950408889634);
+    const int sms = host_sm_count();
+    if (!sms) return TT_ERR_CUDA;
+    // CTAs of a row: as many as fill the GPU's places (two on an SM), while each has 16 KB of the row
+    unsigned ctas = 1;
+    while (ctas < 8 && (size_t)ctas * 2 * n_rows <= (size_t)sms * 2 && n_vocab * score_size(dtype) >= (size_t)ctas * 2 * 16384) ctas *= 2;
+    TT_TRY(dtype == TT_BF16 ? launch_logprobs<__nv_bfloat16>(P, ctas, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs<__half>(P, ctas, (cudaStream_t)stream)
+                            : launch_logprobs<float>(P, ctas, (cudaStream_t)stream));
     return TT_OK;
 }
 

@@ -7,17 +7,18 @@
 #include "tt_host.cuh"
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include <cstring>
 
 constexpr int SCORE_THREADS = 256;
 constexpr int SCORE_TOP_MAX = 32;
 // Below this d the exponential is 0 in 32 bits; it stands for -inf where d is a factor of a product with it.
-constexpr float SCORE_LOW = -1000.0f;
+constexpr float SCORE_LOW = -1000.0f, SCORE_LOW2 = -1500.0f;       // (of the natural exponential, of powers of two)
 
 struct ScoreParams {
     const void* logits;
     unsigned long long n_rows, stride;
     u32 n_vocab, top_k;
-    float scale;
+    float scale, scale2;           // scale2 = scale / ln 2
     const int32_t* ids;
     const long long* ids_off;      // null: row i is asked for ids[i]
     unsigned long long n_docs;
@@ -91,85 +92,365 @@ __device__ __forceinline__ int32_t score_target(const int32_t* ids, unsigned lon
     return id >= 0 && (u32)id < n_vocab ? id : -1;
 }
 
-template <int NT>
-__device__ __forceinline__ float cta_sum(float x, float* buf) {
-    __syncthreads();
-    buf[threadIdx.x] = x;
-    __syncthreads();
-    for (int o = NT / 2; o; o >>= 1) { if ((int)threadIdx.x < o) buf[threadIdx.x] += buf[threadIdx.x + o]; __syncthreads(); }
-    return buf[0];
-}
-// A logit in the order of the entries: larger logits have larger keys, of equal ones the lower index; never 0.
-__device__ __forceinline__ u64 score_key(float x, u32 j) {
+// ---- arithmetic on pairs ------------------------------------------------------------------------------------------
+// Two floats in a 64-bit register: one instruction for both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float a, float b) { f32x2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void pair_to(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 pair_add(f32x2 a, f32x2 b) { f32x2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 pair_mul(f32x2 a, f32x2 b) { f32x2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f32x2 pair_fma(f32x2 a, f32x2 b, f32x2 c) { f32x2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ float exp2_hw(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+
+// A 16-byte vector of a type: its values, its largest one, how many of it are below a pivot.
+template <typename T> struct ScoreVec;
+template <> struct ScoreVec<float> {
+    static constexpr int N = 4;
+    typedef float Pivot;
+    struct Count { u32 n = 0; };
+    __device__ static float at(const uint4& r, int e) { return __uint_as_float(e == 0 ? r.x : e == 1 ? r.y : e == 2 ? r.z : r.w); }
+    __device__ static f32x2 pair(const uint4& r, int p) { return p == 0 ? pair_of(at(r, 0), at(r, 1)) : pair_of(at(r, 2), at(r, 3)); }
+    template <int U> __device__ static float most(const uint4 (&r)[U]) {
+        float m = at(r[0], 0);
+#pragma unroll
+        for (int i = 0; i < U; i++) m = fmaxf(fmaxf(m, fmaxf(at(r[i], 0), at(r[i], 1))), fmaxf(at(r[i], 2), at(r[i], 3)));
+        return m;
+    }
+    __device__ static uint4 lowest() { const u32 w = 0xFF800000u; return make_uint4(w, w, w, w); }
+    __device__ static Pivot pivot(float x) { return x; }
+    // the next larger value
+    __device__ static Pivot above(float x) {
+        const u32 b = __float_as_uint(x + 0.0f);
+        return __uint_as_float(b == 0 ? 1u : b & 0x80000000u ? b - 1 : b + 1);
+    }
+    __device__ static void below(Count& c, const uint4& r, Pivot p) {
+#pragma unroll
+        for (int e = 0; e < N; e++) c.n += at(r, e) < p;
+    }
+    __device__ static u32 take(Count& c) { const u32 n = c.n; c.n = 0; return n; }
+};
+// The 16-bit types: a word is two values; counts are sums of 1.0 in the type itself, exact up to 256.
+template <typename T2> __device__ __forceinline__ T2 as_two(u32 w) { T2 v; memcpy(&v, &w, 4); return v; }
+template <typename T, typename T2, u32 LOWEST> struct ScoreVec16 {
+    static constexpr int N = 8;
+    typedef T2 Pivot;
+    struct Count { T2 n = as_two<T2>(0); };
+    __device__ static u32 word(const uint4& r, int p) { return p == 0 ? r.x : p == 1 ? r.y : p == 2 ? r.z : r.w; }
+    template <int U> __device__ static float most(const uint4 (&r)[U]) {
+        T2 m = as_two<T2>(r[0].x);
+#pragma unroll
+        for (int i = 0; i < U; i++) m = __hmax2(__hmax2(m, __hmax2(as_two<T2>(r[i].x), as_two<T2>(r[i].y))), __hmax2(as_two<T2>(r[i].z), as_two<T2>(r[i].w)));
+        return fmaxf(score_f32(m.x), score_f32(m.y));
+    }
+    __device__ static uint4 lowest() { const u32 w = LOWEST << 16 | LOWEST; return make_uint4(w, w, w, w); }
+    __device__ static Pivot bits_pivot(u32 h) { return as_two<T2>(h << 16 | h); }
+    __device__ static void below(Count& c, const uint4& r, Pivot p) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) c.n = __hadd2(c.n, __hlt2(as_two<T2>(word(r, i)), p));
+    }
+    __device__ static u32 take(Count& c) { const u32 n = (u32)(score_f32(c.n.x) + score_f32(c.n.y)); c.n = as_two<T2>(0); return n; }
+    __device__ static u32 next_bits(u32 b) { return (b & 0x7FFF) == 0 ? 1u : b & 0x8000 ? b - 1 : b + 1; }
+};
+template <> struct ScoreVec<__nv_bfloat16> : ScoreVec16<__nv_bfloat16, __nv_bfloat162, 0xFF80u> {
+    __device__ static float at(const uint4& r, int e) { const u32 w = word(r, e >> 1); return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16); }
+    __device__ static f32x2 pair(const uint4& r, int p) { const u32 w = word(r, p); return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    __device__ static u32 bits(float x) { return __float_as_uint(x) >> 16; }
+    __device__ static Pivot pivot(float x) { return bits_pivot(bits(x)); }
+    __device__ static Pivot above(float x) { return bits_pivot(next_bits(bits(x))); }
+};
+template <> struct ScoreVec<__half> : ScoreVec16<__half, __half2, 0xFC00u> {
+    __device__ static float at(const uint4& r, int e) { const __half2 h = as_two<__half2>(word(r, e >> 1)); return __half2float(e & 1 ? h.y : h.x); }
+    __device__ static f32x2 pair(const uint4& r, int p) { const float2 f = __half22float2(as_two<__half2>(word(r, p))); return pair_of(f.x, f.y); }
+    __device__ static u32 bits(float x) { return __half_as_ushort(__float2half_rn(x)); }
+    __device__ static Pivot pivot(float x) { return bits_pivot(bits(x)); }
+    __device__ static Pivot above(float x) { return bits_pivot(next_bits(bits(x))); }
+};
+
+// The order of the entries as a number: larger logits have larger keys, of equal ones the lower index; never 0.
+__device__ __forceinline__ u32 score_order(float x) {
     const u32 b = __float_as_uint(x + 0.0f);
-    return (u64)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (u32)~j;
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float score_unorder(u32 o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ u64 score_key(float x, u32 j) { return (u64)score_order(x) << 32 | (u32)~j; }
+
+// Largest logit seen and, relative to it and in powers of two, the sums: s of 2^y, u of y 2^y with y = (x - m) c, c = scale / ln 2.
+// m starts at the lowest number, so that rows of -inf leave s = 0 and no difference of infinities arises.
+struct ScoreSum { float m, s, u; };
+constexpr float SCORE_NONE = -3.402823466e38f;
+__device__ __forceinline__ void score_raise(ScoreSum& a, float m, float c) {      // to a reference m >= a.m
+    const float y = (a.m - m) * c, f = exp2_hw(y);
+    a.u = f * fmaf(fmaxf(y, SCORE_LOW2), a.s, a.u);
+    a.s *= f;
+    a.m = m;
 }
 
-// A CTA a row, one pass for the maximum, one for the sums, one for each alternative.
-template <typename T>
-__global__ void __launch_bounds__(SCORE_THREADS)
+// A row goes to a cluster of CTAs, a stretch of its 16-byte vectors to each; thread i of a CTA takes every SCORE_NT-th of them from the i-th
+// on, SCORE_U at a time (a batch).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives
+// each thread also keeps the largest value of its batches, the number of the first batch that has it, and the second largest batch's.  From the
+// 64 largest of 64 groups of threads comes a bound that at least top_k entries reach; what reaches it is then looked up again: in the one
+// batch of each thread whose largest value does, and in the whole share of the few threads with a second batch that does.
+constexpr int SCORE_NT = 512, SCORE_U = 4, SCORE_GROUPS = 64, SCORE_CAND = 1024;
+
+struct ScoreShared {
+    ScoreSum part[SCORE_NT / 32];
+    u32 below[SCORE_NT / 32];
+    ScoreSum sum;                       // of this CTA
+    u32 n_below;
+    u64 bound;
+    u32 n_cand, n_scan;
+    u64 best[SCORE_TOP_MAX];            // of this CTA, in order; 0: it has fewer
+    u64 heads[SCORE_GROUPS];
+    union {
+        u64 keys[SCORE_NT];
+        u64 cand[SCORE_CAND];
+    };
+    u32 scan[SCORE_NT];                 // threads whose whole share is looked up
+    u32 first[SCORE_NT];                // the batch of each thread's largest value
+};
+
+// One CTA's candidates (sh.cand, n of them) in order: the first k to sh.best.
+__device__ __forceinline__ void score_rank(ScoreShared& sh, u32 n, u32 k) {
+    for (u32 i = threadIdx.x; i < n; i += SCORE_NT) {
+        const u64 mine = sh.cand[i];
+        u32 before = 0;
+        for (u32 o = 0; o < n; o++) before += sh.cand[o] > mine;
+        if (before < k) sh.best[before] = mine;
+    }
+}
+
+template <typename T, bool TOP, bool RANK>
+__global__ void __launch_bounds__(SCORE_NT, 2)
 k_logprobs(const __grid_constant__ ScoreParams P) {
-    __shared__ float buf[SCORE_THREADS];
-    __shared__ u64 keys[SCORE_THREADS];
+    typedef ScoreVec<T> V;
+    constexpr int N = V::N, U = SCORE_U, NT = SCORE_NT;
+    __shared__ ScoreShared sh;
     cudaGridDependencySynchronize();
-    if (blockIdx.x == P.n_rows) { score_check<SCORE_THREADS>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
-    const unsigned long long row = blockIdx.x;
-    const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
+    const u32 ctas = cluster_ctas(), cta = cluster_rank();
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    const unsigned long long row = blockIdx.x / ctas;
+    if (row == P.n_rows) { if (cta == 0) score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
     bool in_use;
     const int32_t t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
     if (!in_use) return;
-    const int tid = threadIdx.x;
-    const auto first = [&](u64 below) {                                // the first entry behind the one with key `below`
-        u64 best = 0;
-        for (u32 j = tid; j < P.n_vocab; j += SCORE_THREADS) { const u64 k = score_key(score_f32(x[j]), j); if (k < below && k > best) best = k; }
-        __syncthreads();
-        keys[tid] = best;
-        __syncthreads();
-        for (int o = SCORE_THREADS / 2; o; o >>= 1) { if (tid < o && keys[tid + o] > keys[tid]) keys[tid] = keys[tid + o]; __syncthreads(); }
-        return keys[0];
-    };
-    float m = -INFINITY;
-    for (u32 j = tid; j < P.n_vocab; j += SCORE_THREADS) m = fmaxf(m, score_f32(x[j]));
-    buf[tid] = m;
-    __syncthreads();
-    for (int o = SCORE_THREADS / 2; o; o >>= 1) { if (tid < o) buf[tid] = fmaxf(buf[tid], buf[tid + o]); __syncthreads(); }
-    m = buf[0];
-    const bool nothing = m == -INFINITY;
-    const float ref = nothing ? 0.0f : m, xt = t >= 0 ? score_f32(x[t]) : 0.0f;
-    float s = 0, u = 0;
-    u32 before = 0;
-    for (u32 j = tid; j < P.n_vocab; j += SCORE_THREADS) {
-        const float v = score_f32(x[j]), d = P.scale * (v - ref), e = expf(d);
-        s += e; u += e * fmaxf(d, SCORE_LOW);
-        before += v > xt || (v == xt && (int32_t)j < t);
-    }
-    s = cta_sum<SCORE_THREADS>(s, buf);
-    u = cta_sum<SCORE_THREADS>(u, buf);
-    u32 rank = 0;
-    {
-        u32 w = before;
-        for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(0xFFFFFFFFu, w, o);
-        __syncthreads();
-        if ((tid & 31) == 0) buf[tid >> 5] = __uint_as_float(w);
-        __syncthreads();
-        for (int w2 = 0; w2 < SCORE_THREADS / 32; w2++) rank += __float_as_uint(buf[w2]);
-    }
-    const bool bad = s != s;
-    const float ls = logf(s);
-    if (tid == 0) {
-        P.logprob[row] = t < 0 ? 0.0f : bad ? s : nothing ? -INFINITY : P.scale * (xt - m) - ls;
-        if (P.lse) P.lse[row] = bad ? s : nothing ? -INFINITY : P.scale * m + ls;
-        if (P.entropy) P.entropy[row] = bad ? s : nothing ? 0.0f : ls - u / s;
-        if (P.rank) P.rank[row] = t < 0 || bad ? 0 : (int32_t)(rank + 1);
-    }
-    u64 below = ~0ull;
-    for (u32 k = 0; k < P.top_k; k++) {
-        if (!bad) below = first(below);
-        if (tid == 0) {
-            const u32 j = ~(u32)below;
-            P.top_ids[row * P.top_k + k] = bad ? -1 : (int32_t)j;
-            P.top_lp[row * P.top_k + k] = bad ? s : nothing ? -INFINITY : P.scale * (score_f32(x[j]) - m) - ls;
+    const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
+    // the vectors of the row, between the entries in front of the first 16-byte boundary and those behind the last
+    const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)x & 15)) & 15) / (u32)sizeof(T));
+    const u32 n_vec = (P.n_vocab - lead) / N, behind = P.n_vocab - lead - n_vec * N;
+    const uint4* vec = reinterpret_cast<const uint4*>(x + lead);
+    const u32 v0 = (u32)((u64)n_vec * cta / ctas), v1 = (u32)((u64)n_vec * (cta + 1) / ctas);
+    const float c = P.scale2;
+    const f32x2 c2 = pair_of(c, c);
+    // an entry is before the row's id if it is not (below it, or equal and not in front of it): below `pivot` up to the vector of the id, below the next
+    // larger value behind that vector; the equal ones in the vector itself are added at the end
+    const float xt = t >= 0 ? score_f32(x[t]) : 0.0f;
+    const typename V::Pivot piv0 = V::pivot(xt), piv1 = V::above(xt);
+    const u32 vt = t < (int32_t)lead ? 0 : min(n_vec, ((u32)t - lead) / N) + 1;        // vectors in front of vt: up to the id's
+    ScoreSum a = {SCORE_NONE, 0.0f, 0.0f};
+    u32 n_below = 0;
+    float most1 = -INFINITY, most2 = -INFINITY;
+    u32 first = v0 + tid < v1 ? 0 : 0xFFFFFFFFu;
+    u32 batch = 0;
+    const auto step = [&](const uint4 (&r)[U], u32 v, bool all) {
+        const float bm = V::template most<U>(r);
+        if (TOP) {
+            most2 = fmaxf(most2, fminf(most1, bm));
+            if (bm > most1) { most1 = bm; first = batch; }
         }
+        if (bm > a.m) score_raise(a, bm, c);
+        const f32x2 m2 = pair_of(-a.m, -a.m);
+        f32x2 s2 = pair_of(0.0f, 0.0f), u2 = s2;
+        typename V::Count cnt;
+#pragma unroll
+        for (int i = 0; i < U; i++) {
+            if (!all && v + i * NT >= v1) break;
+#pragma unroll
+            for (int p = 0; p < N / 2; p++) {
+                const f32x2 y = pair_mul(pair_add(V::pair(r[i], p), m2), c2);
+                float y0, y1;
+                pair_to(y, y0, y1);
+                const f32x2 e = pair_of(exp2_hw(y0), exp2_hw(y1));
+                s2 = pair_add(s2, e);
+                u2 = pair_fma(e, pair_of(fmaxf(y0, SCORE_LOW2), fmaxf(y1, SCORE_LOW2)), u2);
+            }
+            if (RANK) V::below(cnt, r[i], v + i * NT < vt ? piv0 : piv1);
+        }
+        float s0, s1, u0, u1;
+        pair_to(s2, s0, s1); pair_to(u2, u0, u1);
+        a.s += s0 + s1; a.u += u0 + u1;
+        if (RANK) n_below += V::take(cnt);
+    };
+    u32 v = v0 + tid;
+    for (; (u64)v + (U - 1) * NT < v1; v += U * NT, batch++) {
+        uint4 r[U];
+#pragma unroll
+        for (int i = 0; i < U; i++) r[i] = __ldg(vec + v + i * NT);
+        step(r, v, true);
+    }
+    if (v < v1) {
+        uint4 r[U];
+#pragma unroll
+        for (int i = 0; i < U; i++) r[i] = v + i * NT < v1 ? __ldg(vec + v + i * NT) : V::lowest();
+        step(r, v, false);
+    }
+    // the entries outside the vectors
+    const u32 loose = cta == 0 ? lead + behind : 0;
+    if ((u32)tid < loose) {
+        const u32 j = (u32)tid < lead ? tid : lead + n_vec * N + (tid - lead);
+        const float e = score_f32(x[j]);
+        if (e > a.m) score_raise(a, e, c);
+        const float y = (e - a.m) * c, w = exp2_hw(y);
+        a.s += w;
+        a.u = fmaf(w, fmaxf(y, SCORE_LOW2), a.u);
+        if (RANK) n_below += e < xt || (e == xt && (int32_t)j >= t);
+    }
+    if (RANK && tid == 32 && t >= 0 && vt > v0 && vt <= v1 && (u32)t >= lead && (u32)t < lead + n_vec * N)
+        for (u32 j = t; j < lead + vt * N; j++) n_below += score_f32(x[j]) == xt;
+    // sums of the CTA
+    float m = a.m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    score_raise(a, m, c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) { a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o); a.u += __shfl_xor_sync(0xFFFFFFFFu, a.u, o); }
+    if (RANK) n_below = __reduce_add_sync(0xFFFFFFFFu, n_below);
+    if (lane == 0) { sh.part[wid] = a; sh.below[wid] = n_below; }
+    if (TOP) {
+        sh.keys[tid] = first == 0xFFFFFFFFu ? 0 : (u64)score_order(most1) << 32 | (u32)~(first * NT + tid);
+        sh.first[tid] = first;
+        if (tid == 0) { sh.bound = 0; sh.n_cand = 0; sh.n_scan = 0; }
+        if (tid < SCORE_TOP_MAX) sh.best[tid] = 0;
+    }
+    __syncthreads();
+    if (wid == NT / 32 - 1) {
+        a = lane < NT / 32 ? sh.part[lane] : ScoreSum{SCORE_NONE, 0.0f, 0.0f};
+        n_below = lane < NT / 32 ? sh.below[lane] : 0;
+        m = a.m;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        score_raise(a, m, c);
+#pragma unroll
+        for (int o = 16; o; o >>= 1) { a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o); a.u += __shfl_xor_sync(0xFFFFFFFFu, a.u, o); }
+        n_below = __reduce_add_sync(0xFFFFFFFFu, n_below);
+        if (lane == 0) { sh.sum = a; sh.n_below = n_below; }
+    }
+    if (TOP) {
+        // the largest entry of every group of threads, by its exact place
+        u64 head = 0;
+        if (tid < SCORE_GROUPS) {
+#pragma unroll
+            for (int q = 0; q < NT / SCORE_GROUPS; q++) head = max(head, sh.keys[tid + q * SCORE_GROUPS]);
+            if (head) {
+                const u32 at = ~(u32)head, w = v0 + at / NT * (U * NT) + at % NT;
+                const float val = score_unorder((u32)(head >> 32));
+                u32 j = lead + w * N;
+                uint4 r[U];
+#pragma unroll
+                for (int i = 0; i < U; i++) r[i] = w + i * NT < v1 ? __ldg(vec + w + i * NT) : V::lowest();
+                bool found = false;
+#pragma unroll
+                for (int i = 0; i < U; i++)
+#pragma unroll
+                    for (int e = 0; e < N; e++)
+                        if (!found && V::at(r[i], e) == val && w + i * NT < v1) { found = true; j = lead + (w + i * NT) * N + e; }
+                head = score_key(val, j);
+            }
+            sh.heads[tid] = head;
+        }
+        __syncthreads();
+        if (tid < SCORE_GROUPS && head) {
+            u32 before = 0;
+#pragma unroll 8
+            for (int o = 0; o < SCORE_GROUPS; o++) before += sh.heads[o] > head;
+            if (before == P.top_k - 1) sh.bound = head;
+        }
+        __syncthreads();
+        while (sh.sum.s == sh.sum.s) {                         // (not where there is a NaN; again only where more entries reach the bound than there is room for: each time with a bound that fewer reach)
+            const u64 bound = sh.bound;
+            const u32 bv = (u32)(bound >> 32), bj = ~(u32)bound;
+            const auto look = [&](const uint4& r, u32 w) {
+#pragma unroll
+                for (int e = 0; e < N; e++) {
+                    const u64 key = score_key(V::at(r, e), lead + w * N + e);
+                    if (key >= bound) { const u32 n = atomicAdd(&sh.n_cand, 1u); if (n < SCORE_CAND) sh.cand[n] = key; }
+                }
+            };
+            if (first != 0xFFFFFFFFu) {
+                const u32 ov = score_order(most1), w = v0 + tid + first * (U * NT);
+                if (bound == 0 || ov > bv || (ov == bv && lead + w * N <= bj)) {
+#pragma unroll
+                    for (int i = 0; i < U; i++) if (w + i * NT < v1) look(__ldg(vec + w + i * NT), w + i * NT);
+                    // others of this thread's batches: all of them, or, where only entries equal to the bound's are left, those in front of it
+                    if (bound == 0 || (score_order(most2) >= bv && (ov > bv || lead + (w + U * NT - tid) * N <= bj))) sh.scan[atomicAdd(&sh.n_scan, 1u)] = tid;
+                }
+            }
+            if ((u32)tid < loose) {
+                const u32 j = (u32)tid < lead ? tid : lead + n_vec * N + (tid - lead);
+                const u64 key = score_key(score_f32(x[j]), j);
+                if (key >= bound) { const u32 n = atomicAdd(&sh.n_cand, 1u); if (n < SCORE_CAND) sh.cand[n] = key; }
+            }
+            __syncthreads();
+            const u32 n_scan = sh.n_scan;
+            for (u32 i = wid; i < n_scan; i += NT / 32) {
+                const u32 o = sh.scan[i], skip = sh.first[o];
+                for (u32 n = lane; (u64)v0 + o + (u64)n * NT < v1; n += 32) if (n / U != skip) look(__ldg(vec + v0 + o + n * NT), v0 + o + n * NT);
+            }
+            __syncthreads();
+            const u32 n_cand = sh.n_cand;
+            score_rank(sh, min(n_cand, (u32)SCORE_CAND), P.top_k);
+            __syncthreads();
+            if (n_cand <= SCORE_CAND) break;
+            if (tid == 0) { sh.bound = sh.best[P.top_k - 1]; sh.n_cand = 0; sh.n_scan = 0; }
+            __syncthreads();
+        }
+    }
+    // the row's from its CTAs'
+    ScoreSum sum;
+    if (ctas > 1) {
+        cluster_sync();
+        if (cta == 0) {
+            if (wid == 0) {
+                ScoreSum b = {SCORE_NONE, 0.0f, 0.0f};
+                u32 nb = 0;
+                if ((u32)lane < ctas) {
+                    const u32 at = cluster_map(&sh.sum, lane);
+                    b.m = cluster_f32(at); b.s = cluster_f32(at + 4); b.u = cluster_f32(at + 8);
+                    nb = __float_as_uint(cluster_f32(cluster_map(&sh.n_below, lane)));
+                }
+                m = b.m;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+                score_raise(b, m, c);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) { b.s += __shfl_xor_sync(0xFFFFFFFFu, b.s, o); b.u += __shfl_xor_sync(0xFFFFFFFFu, b.u, o); }
+                nb = __reduce_add_sync(0xFFFFFFFFu, nb);
+                if (lane == 0) { sh.part[0] = b; sh.below[0] = nb; }
+            }
+            if (TOP) for (u32 i = tid; i < ctas * P.top_k; i += NT) sh.cand[i] = cluster_u64(cluster_map(&sh.best[i % P.top_k], i / P.top_k));
+        }
+        cluster_sync();                                        // (the others' memory is read)
+        if (cta != 0) return;
+        sum = sh.part[0];
+        n_below = sh.below[0];
+        if (TOP) { score_rank(sh, ctas * P.top_k, P.top_k); __syncthreads(); }
+    } else {
+        __syncthreads();
+        sum = sh.sum;
+        n_below = sh.n_below;
+    }
+    const bool bad = sum.s != sum.s, nothing = sum.s == 0.0f;
+    const float ls = logf(sum.s);
+    const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : P.scale * (e - sum.m) - ls; };
+    if (tid == 0) {
+        P.logprob[row] = t < 0 ? 0.0f : log_p(xt);
+        if (P.lse) P.lse[row] = bad ? sum.s : nothing ? -INFINITY : fmaf(P.scale, sum.m, ls);
+        if (P.entropy) P.entropy[row] = bad ? sum.s : nothing ? 0.0f : ls - 0.6931471806f * (sum.u / sum.s);
+        if (RANK) P.rank[row] = t < 0 || bad ? 0 : (int32_t)(P.n_vocab - n_below + 1);
+    }
+    if (TOP && (u32)tid < P.top_k) {
+        const u64 key = sh.best[tid];
+        P.top_ids[row * P.top_k + tid] = bad ? -1 : (int32_t)~(u32)key;
+        P.top_lp[row * P.top_k + tid] = log_p(score_unorder((u32)(key >> 32)));
     }
 }
 

@@ -181,7 +181,7 @@ def test_refusals_without_a_device(tt):
         return L.tt_logprobs(logits, dtype, rows, n, stride, scale, ids, off, docs, k, None, lp, None, None, None, top_i, top_l, status)
 
     bad = [dict(logits=None), dict(logits=a + 1), dict(logits=a + 2, dtype=2), dict(dtype=3), dict(dtype=-1), dict(n=0), dict(n=1 << 31, stride=1 << 31), dict(rows=1 << 24),
-           dict(stride=7), dict(stride=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(ids=None), dict(docs=1),
+           dict(stride=7), dict(stride=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=2.0 ** 101), dict(scale=float("nan")), dict(ids=None), dict(docs=1),
            dict(lp=None), dict(status=None), dict(k=9, top_i=a, top_l=a), dict(k=33, n=64, stride=64, top_i=a, top_l=a), dict(k=1), dict(k=1, top_i=a), dict(top_i=a, top_l=a),
            dict(off=a, docs=1 << 31)]
     for kw in bad:
