@@ -43,6 +43,11 @@ extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t 
     return TT_OK;
 }
 
+template <typename T>
+static cudaError_t launch_logprobs_grad(const ScoreGradParams& P, cudaStream_t st) {
+    return host_launch(P.h ? k_logprobs_grad<T, true> : k_logprobs_grad<T, false>, (unsigned)(P.n_rows * P.parts + 1), SCORE_GRAD_NT, 1, 0, st, P);
+}
+
 extern "C" int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, size_t n_vocab, size_t row_stride, float scale, const int32_t* ids,
                                 const int64_t* ids_off, size_t n_docs, const float* lse, const float* entropy, const float* grad_logprob,
                                 const float* grad_entropy, void* stream, void* grad_out, size_t grad_stride, int32_t* status_out) {
@@ -55,7 +60,14 @@ extern "C" int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, si
     P.logits = logits; P.n_rows = n_rows; P.stride = row_stride; P.grad_stride = grad_stride; P.n_vocab = (u32)n_vocab; P.scale = scale;
     P.ids = ids; P.ids_off = (const long long*)ids_off; P.n_docs = n_docs;
     P.lse = lse; P.entropy = entropy; P.g = grad_logprob; P.h = grad_entropy; P.grad = grad_out; P.status_out = status_out;
-    const auto kernel = dtype == TT_BF16 ? k_logprobs_grad<__nv_bfloat16> : dtype == TT_FP16 ? k_logprobs_grad<__half> : k_logprobs_grad<float>;
-    TT_TRY(host_launch(kernel, (unsigned)n_rows + 1, SCORE_THREADS, 1, 0, (cudaStream_t)stream, P));
+    const int sms = host_sm_count();
+    if (!sms) return TT_ERR_CUDA;
+    // a CTA takes up to four batches of 16 KB, fewer where that leaves places on the GPU (five CTAs on an SM) empty
+    const size_t batch = (size_t)SCORE_GRAD_NT * SCORE_U * 16, bytes = n_vocab * score_size(dtype), places = (size_t)sms * 5;
+    size_t rounds = 4;
+    while (rounds > 1 && n_rows * ((bytes + rounds * batch - 1) / (rounds * batch)) < places) rounds /= 2;
+    P.rounds = (u32)rounds; P.parts = (u32)((bytes + rounds * batch - 1) / (rounds * batch));
+    TT_TRY(dtype == TT_BF16 ? launch_logprobs_grad<__nv_bfloat16>(P, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs_grad<__half>(P, (cudaStream_t)stream)
+                            : launch_logprobs_grad<float>(P, (cudaStream_t)stream));
     return TT_OK;
 }

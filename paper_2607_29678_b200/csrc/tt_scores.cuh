@@ -9,7 +9,6 @@
 #include <cuda_fp16.h>
 #include <cstring>
 
-constexpr int SCORE_THREADS = 256;
 constexpr int SCORE_TOP_MAX = 32;
 // Below this d the exponential is 0 in 32 bits; it stands for -inf where d is a factor of a product with it.
 constexpr float SCORE_LOW = -1000.0f, SCORE_LOW2 = -1500.0f;       // (of the natural exponential, of powers of two)
@@ -29,7 +28,7 @@ struct ScoreParams {
 struct ScoreGradParams {
     const void* logits;
     unsigned long long n_rows, stride, grad_stride;
-    u32 n_vocab;
+    u32 n_vocab, parts, rounds;    // CTAs of a row, batches of each
     float scale;
     const int32_t* ids;
     const long long* ids_off;
@@ -75,20 +74,25 @@ __device__ void score_check(const int32_t* ids, unsigned long long n_rows, u32 n
     else if (threadIdx.x == 0) *status_out = 0;
 }
 
-// The id that row i is asked for, -1 for none; in_use = false: the row is behind the last document.
+// The id that row i is asked for, -1 for none; in_use = false: the row is behind the last document.  Called by whole warps: 32 offsets are
+// looked at in each step of the search (two steps for a thousand documents).
 __device__ __forceinline__ int32_t score_target(const int32_t* ids, unsigned long long n_rows, u32 n_vocab, const long long* off, unsigned long long n_docs, unsigned long long i, bool& in_use) {
-    unsigned long long at = i;
     in_use = true;
-    if (off) {
+    const bool shifted = off != nullptr;
+    int32_t id = !shifted || i + 1 < n_rows ? __ldcg(ids + i + shifted) : -1;
+    if (shifted) {
         const long long total = __ldcg(off + n_docs);
         in_use = total <= (long long)n_rows && (long long)i < total;
         if (!in_use || (long long)(i + 1) >= total) return -1;
-        unsigned long long lo = 0, hi = n_docs;                        // the first offset behind i
-        while (lo < hi) { const unsigned long long mid = (lo + hi) / 2; if (__ldcg(off + mid) <= (long long)i) lo = mid + 1; else hi = mid; }
-        if (__ldcg(off + lo) == (long long)(i + 1)) return -1;         // token i ends its document
-        at = i + 1;
+        unsigned long long lo = 0, hi = n_docs;                        // off[lo] <= i < off[hi]
+        while (hi - lo > 1) {
+            const unsigned long long step = (hi - lo + 31) / 32, at = lo + ((threadIdx.x & 31) + 1) * step;
+            const u32 k = __ffs(__ballot_sync(0xFFFFFFFFu, at >= hi || __ldcg(off + at) > (long long)i)) - 1;
+            hi = min(hi, lo + (k + 1) * step);
+            lo += k * step;
+        }
+        if (__ldcg(off + hi) == (long long)(i + 1)) return -1;         // token i ends its document
     }
-    const int32_t id = __ldcg(ids + at);
     return id >= 0 && (u32)id < n_vocab ? id : -1;
 }
 
@@ -454,25 +458,109 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(SCORE_THREADS)
+// The gradient: with L = scale x_j - lse,  dx_j = exp(L) (A + B L) + [j = t] scale g,  A = -scale (g + h entropy), B = -scale h.
+// Reads a row once and writes it once; a CTA takes a stretch of SCORE_GRAD_NT * SCORE_U * rounds vectors of a row.
+constexpr int SCORE_GRAD_NT = 256;
+
+struct ScoreGradRow { float scale, lse, A, B, hot; int32_t t; };
+template <bool ENT>
+__device__ __forceinline__ void score_grad_pair(const ScoreGradRow& R, f32x2 x, float& a, float& b) {
+    const f32x2 l = pair_fma(x, pair_of(R.scale, R.scale), pair_of(-R.lse, -R.lse)), y = pair_mul(l, pair_of(1.44269504f, 1.44269504f));
+    float y0, y1, l0, l1;
+    pair_to(y, y0, y1);
+    const f32x2 p = pair_of(exp2_hw(y0), exp2_hw(y1));
+    f32x2 f = pair_of(R.A, R.A);
+    if (ENT) { pair_to(l, l0, l1); f = pair_fma(pair_of(R.B, R.B), pair_of(fmaxf(l0, SCORE_LOW), fmaxf(l1, SCORE_LOW)), f); }
+    pair_to(pair_mul(p, f), a, b);
+}
+template <bool ENT>
+__device__ __forceinline__ float score_grad_one(const ScoreGradRow& R, float x, u32 j) {
+    float a, b;
+    score_grad_pair<ENT>(R, pair_of(x, x), a, b);
+    return (int32_t)j == R.t ? a + R.hot : a;
+}
+template <typename T> struct ScorePut;
+template <> struct ScorePut<float> {
+    __device__ static uint4 vec(const float (&v)[4]) { return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])); }
+};
+template <> struct ScorePut<__nv_bfloat16> {
+    __device__ static u32 two(float a, float b) { const __nv_bfloat162 h = __floats2bfloat162_rn(a, b); u32 w; memcpy(&w, &h, 4); return w; }
+    __device__ static uint4 vec(const float (&v)[8]) { return make_uint4(two(v[0], v[1]), two(v[2], v[3]), two(v[4], v[5]), two(v[6], v[7])); }
+};
+template <> struct ScorePut<__half> {
+    __device__ static u32 two(float a, float b) { const __half2 h = __floats2half2_rn(a, b); u32 w; memcpy(&w, &h, 4); return w; }
+    __device__ static uint4 vec(const float (&v)[8]) { return make_uint4(two(v[0], v[1]), two(v[2], v[3]), two(v[4], v[5]), two(v[6], v[7])); }
+};
+
+template <typename T, bool ENT>
+__global__ void __launch_bounds__(SCORE_GRAD_NT, 5)
 k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
+    typedef ScoreVec<T> V;
+    constexpr int N = V::N, U = SCORE_U, NT = SCORE_GRAD_NT;
     cudaGridDependencySynchronize();
-    if (blockIdx.x == P.n_rows) { score_check<SCORE_THREADS>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
-    const unsigned long long row = blockIdx.x;
-    bool in_use;
-    const int32_t t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
-    if (!in_use) return;
+    const unsigned long long row = blockIdx.x / P.parts;
+    const u32 part = blockIdx.x % P.parts, tid = threadIdx.x;
+    if (row == P.n_rows) { score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
     const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
     T* dx = reinterpret_cast<T*>(P.grad) + row * P.grad_stride;
-    const float lse = P.lse[row], ent = P.h ? P.entropy[row] : 0.0f, g = t < 0 ? 0.0f : P.g[row], h = P.h ? P.h[row] : 0.0f;
-    const bool zeros = (g == 0.0f && h == 0.0f) || lse == -INFINITY;
-    for (u32 j = threadIdx.x; j < P.n_vocab; j += SCORE_THREADS) {
-        float v = 0.0f;
-        if (!zeros) {
-            const float lp = fmaf(P.scale, score_f32(x[j]), -lse), p = expf(lp);
-            v = P.scale * (((int32_t)j == t ? g : 0.0f) - p * fmaf(h, fmaxf(lp, SCORE_LOW) + ent, g));
+    ScoreGradRow R;
+    bool in_use;
+    R.t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
+    if (!in_use) return;
+    const float g = R.t < 0 ? 0.0f : P.g[row], h = ENT ? P.h[row] : 0.0f;
+    R.lse = P.lse[row];
+    R.scale = P.scale; R.A = -P.scale * (ENT ? fmaf(h, P.entropy[row], g) : g); R.B = -P.scale * h; R.hot = P.scale * g;
+    const bool zeros = (g == 0.0f && h == 0.0f) || R.lse == -INFINITY;
+    // 16-byte vectors where rows of both lie alike in memory; else the logits are read entry by entry
+    const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)dx & 15)) & 15) / (u32)sizeof(T));
+    const u32 n_vec = (P.n_vocab - lead) / N;
+    const bool alike = (((uintptr_t)x ^ (uintptr_t)dx) & 15) == 0;
+    const u32 share = P.rounds * U * NT;                       // vectors of a CTA
+    uint4* out = reinterpret_cast<uint4*>(dx + lead);
+    const uint4* in = reinterpret_cast<const uint4*>(x + lead);
+    const auto load = [&](u32 v) {
+        if (alike) return __ldcs(in + v);
+        const T* e = x + lead + (size_t)v * N;
+        uint4 r; T w[N];
+#pragma unroll
+        for (int i = 0; i < N; i++) w[i] = e[i];
+        memcpy(&r, w, 16);
+        return r;
+    };
+    const u32 vt = R.t < (int32_t)lead ? 0xFFFFFFFFu : ((u32)R.t - lead) / N;
+    const auto put = [&](const uint4& r, u32 v) {
+        float d[N];
+#pragma unroll
+        for (int p = 0; p < N / 2; p++) score_grad_pair<ENT>(R, V::pair(r, p), d[2 * p], d[2 * p + 1]);
+        if (v == vt) {
+#pragma unroll
+            for (int e = 0; e < N; e++) if ((int32_t)(lead + v * N + e) == R.t) d[e] += R.hot;
         }
-        score_put(dx + j, v);
+        __stcs(out + v, ScorePut<T>::vec(d));
+    };
+    const u32 v1 = (u32)min((u64)n_vec, (u64)(part + 1) * share);
+    u64 v = (u64)part * share + tid;
+    if (zeros) {
+        for (; v < v1; v += NT) __stcs(out + v, make_uint4(0, 0, 0, 0));
+    } else {
+        for (; v + (U - 1) * NT < v1; v += U * NT) {
+            uint4 r[U];
+#pragma unroll
+            for (int i = 0; i < U; i++) r[i] = load((u32)v + i * NT);
+#pragma unroll
+            for (int i = 0; i < U; i++) put(r[i], (u32)v + i * NT);
+        }
+        if (v < v1) {
+            uint4 r[U];
+#pragma unroll
+            for (int i = 0; i < U; i++) if (v + i * NT < v1) r[i] = load((u32)v + i * NT);
+#pragma unroll
+            for (int i = 0; i < U; i++) if (v + i * NT < v1) put(r[i], (u32)v + i * NT);
+        }
+    }
+    const u32 loose = lead + (P.n_vocab - lead - n_vec * N);
+    if (part == 0 && tid < loose) {
+        const u32 j = tid < lead ? tid : n_vec * N + tid;
+        score_put(dx + j, zeros ? 0.0f : score_grad_one<ENT>(R, score_f32(x[j]), j));
     }
 }
