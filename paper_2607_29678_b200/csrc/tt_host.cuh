@@ -37,18 +37,16 @@ static cudaError_t host_launch(void (*kernel)(KernelParams...), unsigned grid, u
 }
 
 #if defined(__CUDACC__)
-// Clusters of CTAs: size, place, barrier (release / acquire), and reads of the shared memory of CTA `rank` at the place of this CTA's `p`.
+// Clusters of CTAs: size, place, barrier (release / acquire), and writes to the shared memory of CTA `rank` at the place of this CTA's `p`.
 __device__ __forceinline__ u32 cluster_ctas() { u32 r; asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r)); return r; }
 __device__ __forceinline__ u32 cluster_rank() { u32 r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ u32 cluster_map(const void* p, u32 rank) {
     u32 r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((u32)__cvta_generic_to_shared(p)), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float cluster_f32(u32 at) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory"); return v; }
-__device__ __forceinline__ u64 cluster_u64(u32 at) { u64 v; asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory"); return v; }
+__device__ __forceinline__ void cluster_put(u32 at, float v) { asm volatile("st.shared::cluster.f32 [%0], %1;" :: "r"(at), "f"(v) : "memory"); }
+__device__ __forceinline__ void cluster_put(u32 at, u64 v) { asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(at), "l"(v) : "memory"); }
 #endif

@@ -35,9 +35,9 @@ extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t 
     P.scale2 = (float)((double)scale * 1.4426950408889634);
     const int sms = host_sm_count();
     if (!sms) return TT_ERR_CUDA;
-    // CTAs of a row: as many as fill the GPU's places (two on an SM), while each has 16 KB of the row
+    // CTAs of a row: as many as fill the GPU's places, while each has 16 KB of the row
     unsigned ctas = 1;
-    while (ctas < 8 && (size_t)ctas * 2 * n_rows <= (size_t)sms * 2 && n_vocab * score_size(dtype) >= (size_t)ctas * 2 * 16384) ctas *= 2;
+    while (ctas < SCORE_CLUSTER && (size_t)ctas * 2 * n_rows <= (size_t)sms * SCORE_CTAS && n_vocab * score_size(dtype) >= (size_t)ctas * 2 * 16384) ctas *= 2;
     TT_TRY(dtype == TT_BF16 ? launch_logprobs<__nv_bfloat16>(P, ctas, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs<__half>(P, ctas, (cudaStream_t)stream)
                             : launch_logprobs<float>(P, ctas, (cudaStream_t)stream));
     return TT_OK;

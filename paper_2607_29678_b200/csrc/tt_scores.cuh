@@ -114,12 +114,10 @@ template <> struct ScoreVec<float> {
     struct Count { u32 n = 0; };
     __device__ static float at(const uint4& r, int e) { return __uint_as_float(e == 0 ? r.x : e == 1 ? r.y : e == 2 ? r.z : r.w); }
     __device__ static f32x2 pair(const uint4& r, int p) { return p == 0 ? pair_of(at(r, 0), at(r, 1)) : pair_of(at(r, 2), at(r, 3)); }
-    template <int U> __device__ static float most(const uint4 (&r)[U]) {
-        float m = at(r[0], 0);
-#pragma unroll
-        for (int i = 0; i < U; i++) m = fmaxf(fmaxf(m, fmaxf(at(r[i], 0), at(r[i], 1))), fmaxf(at(r[i], 2), at(r[i], 3)));
-        return m;
-    }
+    typedef float Most;
+    __device__ static Most most(const uint4& r) { return fmaxf(fmaxf(at(r, 0), at(r, 1)), fmaxf(at(r, 2), at(r, 3))); }
+    __device__ static Most larger(Most a, Most b) { return fmaxf(a, b); }
+    __device__ static float value(Most m) { return m; }
     __device__ static uint4 lowest() { const u32 w = 0xFF800000u; return make_uint4(w, w, w, w); }
     __device__ static Pivot pivot(float x) { return x; }
     // the next larger value
@@ -140,12 +138,10 @@ template <typename T, typename T2, u32 LOWEST> struct ScoreVec16 {
     typedef T2 Pivot;
     struct Count { T2 n = as_two<T2>(0); };
     __device__ static u32 word(const uint4& r, int p) { return p == 0 ? r.x : p == 1 ? r.y : p == 2 ? r.z : r.w; }
-    template <int U> __device__ static float most(const uint4 (&r)[U]) {
-        T2 m = as_two<T2>(r[0].x);
-#pragma unroll
-        for (int i = 0; i < U; i++) m = __hmax2(__hmax2(m, __hmax2(as_two<T2>(r[i].x), as_two<T2>(r[i].y))), __hmax2(as_two<T2>(r[i].z), as_two<T2>(r[i].w)));
-        return fmaxf(score_f32(m.x), score_f32(m.y));
-    }
+    typedef T2 Most;
+    __device__ static Most most(const uint4& r) { return __hmax2(__hmax2(as_two<T2>(r.x), as_two<T2>(r.y)), __hmax2(as_two<T2>(r.z), as_two<T2>(r.w))); }
+    __device__ static Most larger(Most a, Most b) { return __hmax2(a, b); }
+    __device__ static float value(Most m) { return fmaxf(score_f32(m.x), score_f32(m.y)); }
     __device__ static uint4 lowest() { const u32 w = LOWEST << 16 | LOWEST; return make_uint4(w, w, w, w); }
     __device__ static Pivot bits_pivot(u32 h) { return as_two<T2>(h << 16 | h); }
     __device__ static void below(Count& c, const uint4& r, Pivot p) {
@@ -191,10 +187,11 @@ __device__ __forceinline__ void score_raise(ScoreSum& a, float m, float c) {    
 
 // A row goes to a cluster of CTAs, a stretch of its 16-byte vectors to each; thread i of a CTA takes every SCORE_NT-th of them from the i-th
 // on, SCORE_U at a time (a batch).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives
-// each thread also keeps the largest value of its batches, the number of the first batch that has it, and the second largest batch's.  From the
-// 64 largest of 64 groups of threads comes a bound that at least top_k entries reach; what reaches it is then looked up again: in the one
-// batch of each thread whose largest value does, and in the whole share of the few threads with a second batch that does.
-constexpr int SCORE_NT = 512, SCORE_U = 4, SCORE_GROUPS = 64, SCORE_CAND = 1024;
+// each thread also keeps the largest value among its vectors, the first vector that has it, and the largest value of its other batches.  The
+// top_k-th of the largest values of 64 groups of threads, with the end of its vector, is a bound that at least top_k entries reach; what reaches
+// it is then looked up again: in the one batch of each thread whose largest value does, and in the whole share of the few threads with a second
+// batch that does.
+constexpr int SCORE_NT = 256, SCORE_CTAS = 4, SCORE_U = 4, SCORE_GROUPS = 64, SCORE_CAND = 1024, SCORE_CLUSTER = 8;
 
 struct ScoreShared {
     ScoreSum part[SCORE_NT / 32];
@@ -210,33 +207,43 @@ struct ScoreShared {
         u64 cand[SCORE_CAND];
     };
     u32 scan[SCORE_NT];                 // threads whose whole share is looked up
-    u32 first[SCORE_NT];                // the batch of each thread's largest value
+    u32 first[SCORE_NT];                // the vector of each thread's largest value
+    // what the CTAs of a cluster leave with its first one
+    ScoreSum all_sum[SCORE_CLUSTER];
+    u32 all_below[SCORE_CLUSTER];
+    u64 all_best[SCORE_CLUSTER * SCORE_TOP_MAX];
 };
 
-// One CTA's candidates (sh.cand, n of them) in order: the first k to sh.best.
-__device__ __forceinline__ void score_rank(ScoreShared& sh, u32 n, u32 k) {
-    for (u32 i = threadIdx.x; i < n; i += SCORE_NT) {
-        const u64 mine = sh.cand[i];
+// The n distinct keys at `from` in order (0: none), the first k of them to `to`: four threads count what is larger than a key.
+__device__ __forceinline__ void score_rank(const u64* from, u32 n, u64* to, u32 k) {
+    for (u32 i0 = 0; i0 < n; i0 += SCORE_NT / 4) {
+        const u32 i = i0 + threadIdx.x / 4;
+        const u64 mine = i < n ? from[i] : 0;
         u32 before = 0;
-        for (u32 o = 0; o < n; o++) before += sh.cand[o] > mine;
-        if (before < k) sh.best[before] = mine;
+#pragma unroll 4
+        for (u32 o = threadIdx.x % 4; o < n; o += 4) before += from[o] > mine;
+        before += __shfl_xor_sync(0xFFFFFFFFu, before, 1);
+        before += __shfl_xor_sync(0xFFFFFFFFu, before, 2);
+        if (mine && before < k && threadIdx.x % 4 == 0) to[before] = mine;
     }
 }
 
 template <typename T, bool TOP, bool RANK>
-__global__ void __launch_bounds__(SCORE_NT, 2)
+__global__ void __launch_bounds__(SCORE_NT, SCORE_CTAS)
 k_logprobs(const __grid_constant__ ScoreParams P) {
     typedef ScoreVec<T> V;
     constexpr int N = V::N, U = SCORE_U, NT = SCORE_NT;
     __shared__ ScoreShared sh;
-    cudaGridDependencySynchronize();
     const u32 ctas = cluster_ctas(), cta = cluster_rank();
+    if (ctas > 1) cluster_arrive();                            // (the first CTA's memory may be written once it runs)
+    cudaGridDependencySynchronize();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const unsigned long long row = blockIdx.x / ctas;
-    if (row == P.n_rows) { if (cta == 0) score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
-    bool in_use;
-    const int32_t t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
-    if (!in_use) return;
+    bool in_use = false;
+    int32_t t = -1;
+    if (row == P.n_rows) { if (cta == 0) score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); }
+    else t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
+    if (!in_use) { if (ctas > 1) cluster_wait(); return; }
     const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
     // the vectors of the row, between the entries in front of the first 16-byte boundary and those behind the last
     const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)x & 15)) & 15) / (u32)sizeof(T));
@@ -253,13 +260,20 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     ScoreSum a = {SCORE_NONE, 0.0f, 0.0f};
     u32 n_below = 0;
     float most1 = -INFINITY, most2 = -INFINITY;
-    u32 first = v0 + tid < v1 ? 0 : 0xFFFFFFFFu;
-    u32 batch = 0;
+    u32 first = v0 + tid;                                      // (of a thread that has vectors; none of -inf alone is passed over)
     const auto step = [&](const uint4 (&r)[U], u32 v, bool all) {
-        const float bm = V::template most<U>(r);
+        typename V::Most vm[U], h;
+#pragma unroll
+        for (int i = 0; i < U; i++) { vm[i] = V::most(r[i]); h = i ? V::larger(h, vm[i]) : vm[i]; }
+        const float bm = V::value(h);
         if (TOP) {
             most2 = fmaxf(most2, fminf(most1, bm));
-            if (bm > most1) { most1 = bm; first = batch; }
+            if (bm > most1) {
+                most1 = bm;
+                first = v + (U - 1) * NT;
+#pragma unroll
+                for (int i = U - 2; i >= 0; i--) if (V::value(vm[i]) == bm) first = v + i * NT;
+            }
         }
         if (bm > a.m) score_raise(a, bm, c);
         const f32x2 m2 = pair_of(-a.m, -a.m);
@@ -285,7 +299,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         if (RANK) n_below += V::take(cnt);
     };
     u32 v = v0 + tid;
-    for (; (u64)v + (U - 1) * NT < v1; v += U * NT, batch++) {
+    for (; (u64)v + (U - 1) * NT < v1; v += U * NT) {
         uint4 r[U];
 #pragma unroll
         for (int i = 0; i < U; i++) r[i] = __ldg(vec + v + i * NT);
@@ -300,7 +314,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     // the entries outside the vectors
     const u32 loose = cta == 0 ? lead + behind : 0;
     if ((u32)tid < loose) {
-        const u32 j = (u32)tid < lead ? tid : lead + n_vec * N + (tid - lead);
+        const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
         const float e = score_f32(x[j]);
         if (e > a.m) score_raise(a, e, c);
         const float y = (e - a.m) * c, w = exp2_hw(y);
@@ -311,16 +325,20 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     if (RANK && tid == 32 && t >= 0 && vt > v0 && vt <= v1 && (u32)t >= lead && (u32)t < lead + n_vec * N)
         for (u32 j = t; j < lead + vt * N; j++) n_below += score_f32(x[j]) == xt;
     // sums of the CTA
-    float m = a.m;
+    const auto join = [&](ScoreSum& b, u32& nb) {              // over a warp
+        float m = b.m;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-    score_raise(a, m, c);
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        score_raise(b, m, c);
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o); a.u += __shfl_xor_sync(0xFFFFFFFFu, a.u, o); }
-    if (RANK) n_below = __reduce_add_sync(0xFFFFFFFFu, n_below);
+        for (int o = 16; o; o >>= 1) { b.s += __shfl_xor_sync(0xFFFFFFFFu, b.s, o); b.u += __shfl_xor_sync(0xFFFFFFFFu, b.u, o); }
+        if (RANK) nb = __reduce_add_sync(0xFFFFFFFFu, nb);
+    };
+    const bool has = v0 + tid < v1;
+    join(a, n_below);
     if (lane == 0) { sh.part[wid] = a; sh.below[wid] = n_below; }
     if (TOP) {
-        sh.keys[tid] = first == 0xFFFFFFFFu ? 0 : (u64)score_order(most1) << 32 | (u32)~(first * NT + tid);
+        sh.keys[tid] = has ? (u64)score_order(most1) << 32 | (u32)~first : 0;
         sh.first[tid] = first;
         if (tid == 0) { sh.bound = 0; sh.n_cand = 0; sh.n_scan = 0; }
         if (tid < SCORE_TOP_MAX) sh.best[tid] = 0;
@@ -329,47 +347,29 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     if (wid == NT / 32 - 1) {
         a = lane < NT / 32 ? sh.part[lane] : ScoreSum{SCORE_NONE, 0.0f, 0.0f};
         n_below = lane < NT / 32 ? sh.below[lane] : 0;
-        m = a.m;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        score_raise(a, m, c);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) { a.s += __shfl_xor_sync(0xFFFFFFFFu, a.s, o); a.u += __shfl_xor_sync(0xFFFFFFFFu, a.u, o); }
-        n_below = __reduce_add_sync(0xFFFFFFFFu, n_below);
+        join(a, n_below);
         if (lane == 0) { sh.sum = a; sh.n_below = n_below; }
     }
     if (TOP) {
-        // the largest entry of every group of threads, by its exact place
-        u64 head = 0;
+        // the groups' largest values in order: threads 4 i to 4 i + 3 look for the place of group i's
         if (tid < SCORE_GROUPS) {
+            u64 head = 0;
 #pragma unroll
             for (int q = 0; q < NT / SCORE_GROUPS; q++) head = max(head, sh.keys[tid + q * SCORE_GROUPS]);
-            if (head) {
-                const u32 at = ~(u32)head, w = v0 + at / NT * (U * NT) + at % NT;
-                const float val = score_unorder((u32)(head >> 32));
-                u32 j = lead + w * N;
-                uint4 r[U];
-#pragma unroll
-                for (int i = 0; i < U; i++) r[i] = w + i * NT < v1 ? __ldg(vec + w + i * NT) : V::lowest();
-                bool found = false;
-#pragma unroll
-                for (int i = 0; i < U; i++)
-#pragma unroll
-                    for (int e = 0; e < N; e++)
-                        if (!found && V::at(r[i], e) == val && w + i * NT < v1) { found = true; j = lead + (w + i * NT) * N + e; }
-                head = score_key(val, j);
-            }
             sh.heads[tid] = head;
         }
         __syncthreads();
-        if (tid < SCORE_GROUPS && head) {
+        {
+            const u64 head = sh.heads[tid / 4];
             u32 before = 0;
-#pragma unroll 8
-            for (int o = 0; o < SCORE_GROUPS; o++) before += sh.heads[o] > head;
-            if (before == P.top_k - 1) sh.bound = head;
+#pragma unroll
+            for (int o = 0; o < SCORE_GROUPS / 4; o++) before += sh.heads[tid % 4 + 4 * o] > head;
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, 1);
+            before += __shfl_xor_sync(0xFFFFFFFFu, before, 2);
+            if (head && before == P.top_k - 1) sh.bound = score_key(score_unorder((u32)(head >> 32)), lead + ~(u32)head * N + N - 1);
         }
         __syncthreads();
-        while (sh.sum.s == sh.sum.s) {                         // (not where there is a NaN; again only where more entries reach the bound than there is room for: each time with a bound that fewer reach)
+        while (sh.sum.s == sh.sum.s) {                         // (not where there is a NaN; again where more entries reach the bound than there is room for: each time with a bound that fewer reach)
             const u64 bound = sh.bound;
             const u32 bv = (u32)(bound >> 32), bj = ~(u32)bound;
             const auto look = [&](const uint4& r, u32 w) {
@@ -379,68 +379,55 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
                     if (key >= bound) { const u32 n = atomicAdd(&sh.n_cand, 1u); if (n < SCORE_CAND) sh.cand[n] = key; }
                 }
             };
-            if (first != 0xFFFFFFFFu) {
-                const u32 ov = score_order(most1), w = v0 + tid + first * (U * NT);
-                if (bound == 0 || ov > bv || (ov == bv && lead + w * N <= bj)) {
+            const u32 ov = score_order(most1), b0 = (first - v0 - tid) / (U * NT) * (U * NT) + v0;       // the batch: vectors b0 + tid + i * NT
+            const bool hot = has && (bound == 0 || ov > bv || (ov == bv && lead + first * N <= bj));
+            // others of this thread's batches: all of them, or, where only entries equal to the bound's are left, those in front of it
+            if (hot && (bound == 0 || (score_order(most2) >= bv && (ov > bv || lead + (b0 + U * NT) * N <= bj)))) sh.scan[atomicAdd(&sh.n_scan, 1u)] = tid;
+            if (hot) {
+                uint4 r[U];
 #pragma unroll
-                    for (int i = 0; i < U; i++) if (w + i * NT < v1) look(__ldg(vec + w + i * NT), w + i * NT);
-                    // others of this thread's batches: all of them, or, where only entries equal to the bound's are left, those in front of it
-                    if (bound == 0 || (score_order(most2) >= bv && (ov > bv || lead + (w + U * NT - tid) * N <= bj))) sh.scan[atomicAdd(&sh.n_scan, 1u)] = tid;
-                }
+                for (int i = 0; i < U; i++) r[i] = b0 + tid + i * NT < v1 ? __ldg(vec + b0 + tid + i * NT) : V::lowest();
+#pragma unroll
+                for (int i = 0; i < U; i++) if (b0 + tid + i * NT < v1) look(r[i], b0 + tid + i * NT);
             }
             if ((u32)tid < loose) {
-                const u32 j = (u32)tid < lead ? tid : lead + n_vec * N + (tid - lead);
+                const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
                 const u64 key = score_key(score_f32(x[j]), j);
                 if (key >= bound) { const u32 n = atomicAdd(&sh.n_cand, 1u); if (n < SCORE_CAND) sh.cand[n] = key; }
             }
             __syncthreads();
             const u32 n_scan = sh.n_scan;
             for (u32 i = wid; i < n_scan; i += NT / 32) {
-                const u32 o = sh.scan[i], skip = sh.first[o];
+                const u32 o = sh.scan[i], skip = (sh.first[o] - v0 - o) / (U * NT);
                 for (u32 n = lane; (u64)v0 + o + (u64)n * NT < v1; n += 32) if (n / U != skip) look(__ldg(vec + v0 + o + n * NT), v0 + o + n * NT);
             }
             __syncthreads();
             const u32 n_cand = sh.n_cand;
-            score_rank(sh, min(n_cand, (u32)SCORE_CAND), P.top_k);
+            score_rank(sh.cand, min(n_cand, (u32)SCORE_CAND), sh.best, P.top_k);
             __syncthreads();
             if (n_cand <= SCORE_CAND) break;
             if (tid == 0) { sh.bound = sh.best[P.top_k - 1]; sh.n_cand = 0; sh.n_scan = 0; }
             __syncthreads();
         }
-    }
+    } else __syncthreads();
     // the row's from its CTAs'
-    ScoreSum sum;
+    ScoreSum sum = sh.sum;
+    n_below = sh.n_below;
     if (ctas > 1) {
-        cluster_sync();
-        if (cta == 0) {
-            if (wid == 0) {
-                ScoreSum b = {SCORE_NONE, 0.0f, 0.0f};
-                u32 nb = 0;
-                if ((u32)lane < ctas) {
-                    const u32 at = cluster_map(&sh.sum, lane);
-                    b.m = cluster_f32(at); b.s = cluster_f32(at + 4); b.u = cluster_f32(at + 8);
-                    nb = __float_as_uint(cluster_f32(cluster_map(&sh.n_below, lane)));
-                }
-                m = b.m;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-                score_raise(b, m, c);
-#pragma unroll
-                for (int o = 16; o; o >>= 1) { b.s += __shfl_xor_sync(0xFFFFFFFFu, b.s, o); b.u += __shfl_xor_sync(0xFFFFFFFFu, b.u, o); }
-                nb = __reduce_add_sync(0xFFFFFFFFu, nb);
-                if (lane == 0) { sh.part[0] = b; sh.below[0] = nb; }
-            }
-            if (TOP) for (u32 i = tid; i < ctas * P.top_k; i += NT) sh.cand[i] = cluster_u64(cluster_map(&sh.best[i % P.top_k], i / P.top_k));
+        cluster_wait();
+        if (tid == 0) {
+            const u32 at = cluster_map(&sh.all_sum[cta], 0);
+            cluster_put(at, sum.m); cluster_put(at + 4, sum.s); cluster_put(at + 8, sum.u);
+            cluster_put(cluster_map(&sh.all_below[cta], 0), __uint_as_float(n_below));
         }
-        cluster_sync();                                        // (the others' memory is read)
+        if (TOP && (u32)tid < P.top_k) cluster_put(cluster_map(&sh.all_best[cta * P.top_k + tid], 0), sh.best[tid]);
+        cluster_arrive();
+        cluster_wait();
         if (cta != 0) return;
-        sum = sh.part[0];
-        n_below = sh.below[0];
-        if (TOP) { score_rank(sh, ctas * P.top_k, P.top_k); __syncthreads(); }
-    } else {
-        __syncthreads();
-        sum = sh.sum;
-        n_below = sh.n_below;
+        sum = (u32)lane < ctas ? sh.all_sum[lane] : ScoreSum{SCORE_NONE, 0.0f, 0.0f};
+        n_below = (u32)lane < ctas ? sh.all_below[lane] : 0;
+        join(sum, n_below);
+        if (TOP) { score_rank(sh.all_best, ctas * P.top_k, sh.best, P.top_k); __syncthreads(); }
     }
     const bool bad = sum.s != sum.s, nothing = sum.s == 0.0f;
     const float ls = logf(sum.s);
