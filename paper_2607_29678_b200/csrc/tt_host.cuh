@@ -37,9 +37,11 @@ static cudaError_t host_launch(void (*kernel)(KernelParams...), unsigned grid, u
 }
 
 #if defined(__CUDACC__)
-// Clusters of CTAs: size, place, barrier (release / acquire), and writes to the shared memory of CTA `rank` at the place of this CTA's `p`.
-__device__ __forceinline__ u32 cluster_ctas() { u32 r; asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(r)); return r; }
-__device__ __forceinline__ u32 cluster_rank() { u32 r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+// 16 bytes from device to shared memory, both aligned to 16, on their way until the thread has waited for all but the last N of its groups.
+__device__ __forceinline__ void copy_async(void* to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"((u32)__cvta_generic_to_shared(to)), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
+// Clusters of CTAs: barrier (release / acquire), and writes to the shared memory of CTA `rank` at the place of this CTA's `p`.
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ u32 cluster_map(const void* p, u32 rank) {

@@ -14,10 +14,26 @@ static int score_args(const void* logits, int dtype, size_t n_rows, size_t n_voc
     return TT_OK;
 }
 
+template <typename T, int NT>
+static cudaError_t launch_logprobs_nt(const ScoreParams& P, cudaStream_t st) {
+    const auto kernel = P.top_k ? (P.rank ? k_logprobs<T, true, true, NT> : k_logprobs<T, true, false, NT>) : P.rank ? k_logprobs<T, false, true, NT> : k_logprobs<T, false, false, NT>;
+    return host_launch(kernel, ((unsigned)P.n_rows + 1) << P.log_ctas, NT, 1u << P.log_ctas, 0, st, P);
+}
+// Threads of a CTA and CTAs of a row.  An SM has places for SCORE_PLACES threads.
+//   Short rows, many of them: CTAs of 64 (4,096 rows of 8.7 KB: 64 threads 17 us, with alternatives 32, 128 threads 23 and 38, 256 39 and 59).
+//   Otherwise 128 threads where the rows alone fill the GPU (4,096 rows of 200 KB: 64 threads 139 us, 128 133, 256 141; with alternatives 218,
+//   169, 182), but for a second round that would be less than half full, which 64 threads avoid (1,000 rows of 400 KB: 66, 90, 74).
+//   Fewer rows: up to one for each SM 256 threads, else 128, and a cluster for a row as long as its CTAs have places and 48 KB each
+//   (one row of 200 KB: 1 CTA 11.6 us, 4 7.7; 64 rows of 400 KB: 1 CTA 21, 4 14.9, 8 24; 300 of 400 KB: 42, of 2 CTAs 36, 4 37, 8 46;
+//   64 rows of 64 KB: 1 CTA 8.8, 2 9.2, 8 15.7).
 template <typename T>
-static cudaError_t launch_logprobs(const ScoreParams& P, unsigned ctas, cudaStream_t st) {
-    const auto kernel = P.top_k ? (P.rank ? k_logprobs<T, true, true> : k_logprobs<T, true, false>) : P.rank ? k_logprobs<T, false, true> : k_logprobs<T, false, false>;
-    return host_launch(kernel, ((unsigned)P.n_rows + 1) * ctas, SCORE_NT, ctas, 0, st, P);
+static cudaError_t launch_logprobs(ScoreParams& P, size_t sms, cudaStream_t st) {
+    const size_t bytes = (size_t)P.n_vocab * sizeof(T), places = sms * SCORE_PLACES;
+    P.log_ctas = 0;
+    if ((bytes <= 16384 && P.n_rows > places / 256) || (P.n_rows > places / 128 && P.n_rows <= places / 128 * 3 / 2)) return launch_logprobs_nt<T, 64>(P, st);
+    const size_t nt = P.n_rows <= sms ? 256 : 128;
+    while (2u << P.log_ctas <= SCORE_CLUSTER && (P.n_rows * nt << (P.log_ctas + 1)) <= places && bytes >> (P.log_ctas + 1) >= 49152) P.log_ctas++;
+    return nt == 256 ? launch_logprobs_nt<T, 256>(P, st) : launch_logprobs_nt<T, 128>(P, st);
 }
 
 extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t n_vocab, size_t row_stride, float scale, const int32_t* ids,
@@ -35,11 +51,8 @@ extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t 
     P.scale2 = (float)((double)scale * 1.4426950408889634);
     const int sms = host_sm_count();
     if (!sms) return TT_ERR_CUDA;
-    // CTAs of a row: as many as fill the GPU's places, while each has 16 KB of the row
-    unsigned ctas = 1;
-    while (ctas < SCORE_CLUSTER && (size_t)ctas * 2 * n_rows <= (size_t)sms * SCORE_CTAS && n_vocab * score_size(dtype) >= (size_t)ctas * 2 * 16384) ctas *= 2;
-    TT_TRY(dtype == TT_BF16 ? launch_logprobs<__nv_bfloat16>(P, ctas, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs<__half>(P, ctas, (cudaStream_t)stream)
-                            : launch_logprobs<float>(P, ctas, (cudaStream_t)stream));
+    TT_TRY(dtype == TT_BF16 ? launch_logprobs<__nv_bfloat16>(P, sms, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs<__half>(P, sms, (cudaStream_t)stream)
+                            : launch_logprobs<float>(P, sms, (cudaStream_t)stream));
     return TT_OK;
 }
 

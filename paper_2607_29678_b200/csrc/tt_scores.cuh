@@ -16,7 +16,7 @@ constexpr float SCORE_LOW = -1000.0f, SCORE_LOW2 = -1500.0f;       // (of the na
 struct ScoreParams {
     const void* logits;
     unsigned long long n_rows, stride;
-    u32 n_vocab, top_k;
+    u32 n_vocab, top_k, log_ctas;  // CTAs of a row: 2^log_ctas
     float scale, scale2;           // scale2 = scale / ln 2
     const int32_t* ids;
     const long long* ids_off;      // null: row i is asked for ids[i]
@@ -45,55 +45,86 @@ __device__ __forceinline__ void score_put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void score_put(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void score_put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
-// The status of the call, by one CTA: the offsets, and the ids that rows are asked for.
+// The status of the call, by one CTA (the first, so that it runs beside the rows): the offsets, and the ids that rows are asked for.  Eight loads
+// of a thread are on their way at once.
 template <int NT>
 __device__ void score_check(const int32_t* ids, unsigned long long n_rows, u32 n_vocab, const long long* off, unsigned long long n_docs, int32_t* status_out) {
+    constexpr int AT_ONCE = 8;
     bool bad_off = false, bad_id = false;
     unsigned long long total = n_rows;
     if (off) {
         const long long t = __ldcg(off + n_docs);
-        for (unsigned long long d = threadIdx.x; d < n_docs; d += NT) bad_off |= __ldcg(off + d) > __ldcg(off + d + 1);
-        bad_off |= __ldcg(off) != 0 || t < 0;
         if (t > 0 && (unsigned long long)t > n_rows) { if (threadIdx.x == 0) *status_out = 5 /* TT_ERR_CAPACITY */; return; }
+        for (unsigned long long d0 = threadIdx.x; d0 < n_docs; d0 += NT * AT_ONCE) {
+            long long a[AT_ONCE], b[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i++) {
+                const unsigned long long d = d0 + i * NT;
+                a[i] = d < n_docs ? __ldcg(off + d) : 0;
+                b[i] = d < n_docs ? __ldcg(off + d + 1) : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; i++) bad_off |= a[i] > b[i];
+        }
+        bad_off |= __ldcg(off) != 0 || t < 0;
         total = t < 0 ? 0 : (unsigned long long)t;
     }
     if (__syncthreads_or(bad_off)) { if (threadIdx.x == 0) *status_out = 1 /* TT_ERR_ARG */; return; }
     // the first id of a document is asked for by no row: of the others, each that is out of range counts
-    for (unsigned long long i = threadIdx.x; i < total; i += NT) {
-        const int32_t id = __ldcg(ids + i);
-        if (off ? (u32)id < n_vocab : id < (long long)n_vocab) continue;
-        bool asked = true;
-        if (off) {
-            unsigned long long lo = 0, hi = n_docs;                    // is i the beginning of a document?
-            while (lo < hi) { const unsigned long long mid = (lo + hi) / 2; if (__ldcg(off + mid) < (long long)i) lo = mid + 1; else hi = mid; }
-            asked = __ldcg(off + lo) != (long long)i;
+    for (unsigned long long i0 = threadIdx.x; i0 < total; i0 += NT * AT_ONCE) {
+        int32_t id[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; k++) id[k] = i0 + k * NT < total ? __ldcg(ids + i0 + k * NT) : 0;
+        bool any = false;
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; k++) any |= off ? (u32)id[k] >= n_vocab : id[k] >= (long long)n_vocab;
+        if (any && !bad_id) {
+            for (int k = 0; k < AT_ONCE; k++) {
+                const unsigned long long i = i0 + k * NT;
+                if (i >= total) break;
+                const int32_t x = __ldcg(ids + i);
+                if (off ? (u32)x < n_vocab : x < (long long)n_vocab) continue;
+                bool asked = true;
+                if (off) {
+                    unsigned long long lo = 0, hi = n_docs;            // is i the beginning of a document?
+                    while (lo < hi) { const unsigned long long mid = (lo + hi) / 2; if (__ldcg(off + mid) < (long long)i) lo = mid + 1; else hi = mid; }
+                    asked = __ldcg(off + lo) != (long long)i;
+                }
+                bad_id |= asked;
+            }
         }
-        bad_id |= asked;
     }
     if (__syncthreads_or(bad_id)) { if (threadIdx.x == 0) *status_out = 8 /* TT_ERR_BAD_IDS */; }
     else if (threadIdx.x == 0) *status_out = 0;
 }
 
-// The id that row i is asked for, -1 for none; in_use = false: the row is behind the last document.  Called by whole warps: 32 offsets are
-// looked at in each step of the search (two steps for a thousand documents).
-__device__ __forceinline__ int32_t score_target(const int32_t* ids, unsigned long long n_rows, u32 n_vocab, const long long* off, unsigned long long n_docs, unsigned long long i, bool& in_use) {
-    in_use = true;
+// The id that row i is asked for, -1 for none, and its logit; in_use = false: the row is behind the last document.  Called by whole warps: 32
+// offsets are looked at in each step of the search (two steps for a thousand documents), while the id and its logit are on their way.
+template <typename T>
+__device__ __forceinline__ int32_t score_target(const int32_t* ids, unsigned long long n_rows, u32 n_vocab, const long long* off, unsigned long long n_docs, unsigned long long i,
+                                                const T* x, bool& in_use, float& xt) {
     const bool shifted = off != nullptr;
     int32_t id = !shifted || i + 1 < n_rows ? __ldcg(ids + i + shifted) : -1;
+    if (id < 0 || (u32)id >= n_vocab) id = -1;
+    xt = x && id >= 0 ? score_f32(x[id]) : INFINITY;
+    in_use = true;
     if (shifted) {
         const long long total = __ldcg(off + n_docs);
-        in_use = total <= (long long)n_rows && (long long)i < total;
-        if (!in_use || (long long)(i + 1) >= total) return -1;
-        unsigned long long lo = 0, hi = n_docs;                        // off[lo] <= i < off[hi]
+        long long end = total;                                         // off[hi]
+        unsigned long long lo = 0, hi = n_docs;                        // off[lo] <= i < off[hi], if the row is in use
         while (hi - lo > 1) {
             const unsigned long long step = (hi - lo + 31) / 32, at = lo + ((threadIdx.x & 31) + 1) * step;
-            const u32 k = __ffs(__ballot_sync(0xFFFFFFFFu, at >= hi || __ldcg(off + at) > (long long)i)) - 1;
+            const long long o = at >= hi ? end : __ldcg(off + at);
+            const u32 k = __ffs(__ballot_sync(0xFFFFFFFFu, at >= hi || o > (long long)i)) - 1;
+            end = __shfl_sync(0xFFFFFFFFu, o, k);
             hi = min(hi, lo + (k + 1) * step);
             lo += k * step;
         }
-        if (__ldcg(off + hi) == (long long)(i + 1)) return -1;         // token i ends its document
+        in_use = total <= (long long)n_rows && (long long)i < total;
+        if ((long long)(i + 1) >= total || end == (long long)(i + 1)) id = -1;       // token i ends its document
+        if (id < 0) xt = INFINITY;
     }
-    return id >= 0 && (u32)id < n_vocab ? id : -1;
+    return id;
 }
 
 // ---- arithmetic on pairs ------------------------------------------------------------------------------------------
@@ -174,34 +205,52 @@ __device__ __forceinline__ u32 score_order(float x) {
 __device__ __forceinline__ float score_unorder(u32 o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }
 __device__ __forceinline__ u64 score_key(float x, u32 j) { return (u64)score_order(x) << 32 | (u32)~j; }
 
-// Largest logit seen and, relative to it and in powers of two, the sums: s of 2^y, u of y 2^y with y = (x - m) c, c = scale / ln 2.
+// Largest logit m seen and, relative to it and in powers of two, the sums: s of 2^y, u of y 2^y with y = x c - M, c = scale / ln 2, M = m c
+// rounded, which is one multiply-add for each logit and pair of sums.  What the rounding of M leaves, rho = M - m c, takes part in every step
+// from one m to another, so that nothing is lost by it.  Where m c is too large for that (a row of the type's lowest value), M is a NaN and rho 0: the sums of such a batch are
+// NaNs, and it is worked out again as y = (x - m) c - rho, as are batches with a y of -inf (masked logits), whose product with 2^y is a NaN.
 // m starts at the lowest number, so that rows of -inf leave s = 0 and no difference of infinities arises.
 struct ScoreSum { float m, s, u; };
-constexpr float SCORE_NONE = -3.402823466e38f;
+constexpr float SCORE_NONE = -3.402823466e38f, SCORE_LARGE = 1e30f;
+__device__ __forceinline__ float score_ref(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? M : NAN; }
+__device__ __forceinline__ float score_rho(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? -fmaf(m, c, -M) : 0.0f; }
 __device__ __forceinline__ void score_raise(ScoreSum& a, float m, float c) {      // to a reference m >= a.m
-    const float y = (a.m - m) * c, f = exp2_hw(y);
+    const float y = fmaf(a.m - m, c, score_rho(a.m, c) - score_rho(m, c)), f = exp2_hw(y);
     a.u = f * fmaf(fmaxf(y, SCORE_LOW2), a.s, a.u);
     a.s *= f;
     a.m = m;
 }
 
+// A vector's terms, for any logits.
+template <typename V>
+__device__ __forceinline__ void score_add(const uint4& r, float m, float c, float rho, float& s, float& u) {
+#pragma unroll
+    for (int e = 0; e < V::N; e++) {
+        const float y = fmaf(V::at(r, e) - m, c, -rho), w = exp2_hw(y);
+        s += w;
+        u = fmaf(w, fmaxf(y, SCORE_LOW2), u);
+    }
+}
+
 // A row goes to a cluster of CTAs, a stretch of its 16-byte vectors to each; thread i of a CTA takes every SCORE_NT-th of them from the i-th
-// on, SCORE_U at a time (a batch).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives
+// on, SCORE_U at a time (a batch); SCORE_PLACES threads of 80 registers are on an SM at once (with 64, 1,024 of them,
+// the loop spills: 4,096 rows of 100,256 16-bit logits with alternatives 252 us, so 176).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives
 // each thread also keeps the largest value among its vectors, the first vector that has it, and the largest value of its other batches.  The
 // top_k-th of the largest values of 64 groups of threads, with the end of its vector, is a bound that at least top_k entries reach; what reaches
 // it is then looked up again: in the one batch of each thread whose largest value does, and in the whole share of the few threads with a second
 // batch that does.
-constexpr int SCORE_NT = 256, SCORE_CTAS = 4, SCORE_U = 4, SCORE_GROUPS = 64, SCORE_CAND = 1024, SCORE_CLUSTER = 8;
+constexpr int SCORE_U = 4, SCORE_CAND = 512, SCORE_CLUSTER = 8, SCORE_PLACES = 768;
 
+template <int SCORE_NT>
 struct ScoreShared {
     ScoreSum part[SCORE_NT / 32];
-    u32 below[SCORE_NT / 32];
+    u32 before[SCORE_NT / 32];
     ScoreSum sum;                       // of this CTA
-    u32 n_below;
+    u32 n_before;
     u64 bound;
     u32 n_cand, n_scan;
     u64 best[SCORE_TOP_MAX];            // of this CTA, in order; 0: it has fewer
-    u64 heads[SCORE_GROUPS];
+    u64 heads[64];
     union {
         u64 keys[SCORE_NT];
         u64 cand[SCORE_CAND];
@@ -210,11 +259,12 @@ struct ScoreShared {
     u32 first[SCORE_NT];                // the vector of each thread's largest value
     // what the CTAs of a cluster leave with its first one
     ScoreSum all_sum[SCORE_CLUSTER];
-    u32 all_below[SCORE_CLUSTER];
+    u32 all_before[SCORE_CLUSTER];
     u64 all_best[SCORE_CLUSTER * SCORE_TOP_MAX];
 };
 
 // The n distinct keys at `from` in order (0: none), the first k of them to `to`: four threads count what is larger than a key.
+template <int SCORE_NT>
 __device__ __forceinline__ void score_rank(const u64* from, u32 n, u64* to, u32 k) {
     for (u32 i0 = 0; i0 < n; i0 += SCORE_NT / 4) {
         const u32 i = i0 + threadIdx.x / 4;
@@ -228,88 +278,124 @@ __device__ __forceinline__ void score_rank(const u64* from, u32 n, u64* to, u32 
     }
 }
 
-template <typename T, bool TOP, bool RANK>
-__global__ void __launch_bounds__(SCORE_NT, SCORE_CTAS)
+template <typename T, bool TOP, bool RANK, int NT>
+__global__ void __launch_bounds__(NT, SCORE_PLACES / NT)
 k_logprobs(const __grid_constant__ ScoreParams P) {
     typedef ScoreVec<T> V;
-    constexpr int N = V::N, U = SCORE_U, NT = SCORE_NT;
-    __shared__ ScoreShared sh;
-    const u32 ctas = cluster_ctas(), cta = cluster_rank();
+    constexpr int N = V::N, U = SCORE_U, GROUPS = NT < 64 ? NT : 64;
+    __shared__ ScoreShared<NT> sh;
+    __shared__ uint4 ring[2][U][NT];
+    const u32 ctas = 1u << P.log_ctas, cta = blockIdx.x & (ctas - 1);
     if (ctas > 1) cluster_arrive();                            // (the first CTA's memory may be written once it runs)
     cudaGridDependencySynchronize();
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const unsigned long long row = blockIdx.x / ctas;
-    bool in_use = false;
-    int32_t t = -1;
-    if (row == P.n_rows) { if (cta == 0) score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); }
-    else t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
-    if (!in_use) { if (ctas > 1) cluster_wait(); return; }
+    const unsigned long long row = (unsigned long long)(blockIdx.x >> P.log_ctas) - 1;
+    if (blockIdx.x < ctas) {
+        if (cta == 0) score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out);
+        if (ctas > 1) cluster_wait();
+        return;
+    }
     const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
     // the vectors of the row, between the entries in front of the first 16-byte boundary and those behind the last
     const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)x & 15)) & 15) / (u32)sizeof(T));
     const u32 n_vec = (P.n_vocab - lead) / N, behind = P.n_vocab - lead - n_vec * N;
     const uint4* vec = reinterpret_cast<const uint4*>(x + lead);
-    const u32 v0 = (u32)((u64)n_vec * cta / ctas), v1 = (u32)((u64)n_vec * (cta + 1) / ctas);
+    const u32 v0 = (u32)((u64)n_vec * cta >> P.log_ctas), v1 = (u32)((u64)n_vec * (cta + 1) >> P.log_ctas);
+    // Two batches are on their way to the thread's own places in shared memory, so that the loads of one run under the arithmetic of the other (and
+    // the first two while the row's id is looked up).
+    const auto fetch = [&](u32 stage, u64 v) {
+#pragma unroll
+        for (int i = 0; i < U; i++) if (v + i * NT < v1) copy_async(&ring[stage][i][tid], vec + v + i * NT);
+        copy_commit();
+    };
+    fetch(0, v0 + tid);
+    fetch(1, (u64)v0 + tid + U * NT);
+    bool in_use;
+    float xt;
+    const int32_t t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, x, in_use, xt);
+    if (!in_use) { if (ctas > 1) cluster_wait(); return; }
     const float c = P.scale2;
     const f32x2 c2 = pair_of(c, c);
-    // an entry is before the row's id if it is not (below it, or equal and not in front of it): below `pivot` up to the vector of the id, below the next
-    // larger value behind that vector; the equal ones in the vector itself are added at the end
-    const float xt = t >= 0 ? score_f32(x[t]) : 0.0f;
-    const typename V::Pivot piv0 = V::pivot(xt), piv1 = V::above(xt);
-    const u32 vt = t < (int32_t)lead ? 0 : min(n_vec, ((u32)t - lead) / N) + 1;        // vectors in front of vt: up to the id's
+    // entries before the row's id: those not below it in the vectors in front of the id's, those not below the next larger value in the others;
+    // equal ones in front of it in its own vector are added at the end
+    const u32 vt = t < (int32_t)lead ? 0 : min(n_vec, ((u32)t - lead) / N);
     ScoreSum a = {SCORE_NONE, 0.0f, 0.0f};
-    u32 n_below = 0;
+    float ref = NAN;
+    u32 n_before = 0;
     float most1 = -INFINITY, most2 = -INFINITY;
     u32 first = v0 + tid;                                      // (of a thread that has vectors; none of -inf alone is passed over)
-    const auto step = [&](const uint4 (&r)[U], u32 v, bool all) {
+    const auto top = [&](float bm) {                           // a batch's largest value: does it raise the thread's?
+        most2 = fmaxf(most2, fminf(most1, bm));
+        const bool up = bm > most1;
+        if (up) most1 = bm;
+        return up;
+    };
+    u32 stage = 0, v = v0 + tid;
+    for (; (u64)v + (U - 1) * NT < v1; v += U * NT, stage ^= 1) {
+        copy_wait<1>();
+        uint4 r[U];
         typename V::Most vm[U], h;
 #pragma unroll
-        for (int i = 0; i < U; i++) { vm[i] = V::most(r[i]); h = i ? V::larger(h, vm[i]) : vm[i]; }
+        for (int i = 0; i < U; i++) { r[i] = ring[stage][i][tid]; vm[i] = V::most(r[i]); h = i ? V::larger(h, vm[i]) : vm[i]; }
         const float bm = V::value(h);
-        if (TOP) {
-            most2 = fmaxf(most2, fminf(most1, bm));
-            if (bm > most1) {
-                most1 = bm;
-                first = v + (U - 1) * NT;
+        asm volatile("" :: "f"(bm) : "memory");                // (all of the batch is in registers: its place is free)
+        fetch(stage, (u64)v + 2 * U * NT);
+        if (TOP && top(bm)) {
+            first = v + (U - 1) * NT;
 #pragma unroll
-                for (int i = U - 2; i >= 0; i--) if (V::value(vm[i]) == bm) first = v + i * NT;
-            }
+            for (int i = U - 2; i >= 0; i--) if (V::value(vm[i]) == bm) first = v + i * NT;
         }
-        if (bm > a.m) score_raise(a, bm, c);
-        const f32x2 m2 = pair_of(-a.m, -a.m);
+        if (bm > a.m) { score_raise(a, bm, c); ref = score_ref(bm, c); }
+        const f32x2 ref2 = pair_of(-ref, -ref);
         f32x2 s2 = pair_of(0.0f, 0.0f), u2 = s2;
-        typename V::Count cnt;
 #pragma unroll
         for (int i = 0; i < U; i++) {
-            if (!all && v + i * NT >= v1) break;
 #pragma unroll
             for (int p = 0; p < N / 2; p++) {
-                const f32x2 y = pair_mul(pair_add(V::pair(r[i], p), m2), c2);
+                const f32x2 y = pair_fma(V::pair(r[i], p), c2, ref2);
                 float y0, y1;
                 pair_to(y, y0, y1);
                 const f32x2 e = pair_of(exp2_hw(y0), exp2_hw(y1));
                 s2 = pair_add(s2, e);
-                u2 = pair_fma(e, pair_of(fmaxf(y0, SCORE_LOW2), fmaxf(y1, SCORE_LOW2)), u2);
+                u2 = pair_fma(e, y, u2);
             }
-            if (RANK) V::below(cnt, r[i], v + i * NT < vt ? piv0 : piv1);
         }
         float s0, s1, u0, u1;
         pair_to(s2, s0, s1); pair_to(u2, u0, u1);
-        a.s += s0 + s1; a.u += u0 + u1;
-        if (RANK) n_below += V::take(cnt);
-    };
-    u32 v = v0 + tid;
-    for (; (u64)v + (U - 1) * NT < v1; v += U * NT) {
-        uint4 r[U];
+        s0 += s1; u0 += u1;
+        if (u0 != u0) {                                        // masked logits, or some beyond the range of a product
+            s0 = u0 = 0.0f;
+            const float rho = score_rho(a.m, c);
 #pragma unroll
-        for (int i = 0; i < U; i++) r[i] = __ldg(vec + v + i * NT);
-        step(r, v, true);
+            for (int i = 0; i < U; i++) score_add<V>(r[i], a.m, c, rho, s0, u0);
+        }
+        a.s += s0; a.u += u0;
+        if (RANK && bm >= xt) {
+            const typename V::Pivot piv0 = V::pivot(xt), piv1 = V::above(xt);
+            typename V::Count cnt;
+#pragma unroll
+            for (int i = 0; i < U; i++) V::below(cnt, r[i], v + i * NT < vt ? piv0 : piv1);
+            n_before += U * N - V::take(cnt);
+        }
     }
-    if (v < v1) {
-        uint4 r[U];
-#pragma unroll
-        for (int i = 0; i < U; i++) r[i] = v + i * NT < v1 ? __ldg(vec + v + i * NT) : V::lowest();
-        step(r, v, false);
+    if (v < v1) {                                              // the last batch, vector by vector
+        copy_wait<1>();
+        float bm = -INFINITY;
+#pragma unroll 1
+        for (u32 i = 0, w = v; w < v1; i++, w += NT) {
+            const uint4 r = ring[stage][i][tid];
+            const float vm = V::value(V::most(r));
+            if (TOP && vm > fmaxf(most1, bm)) first = w;
+            bm = fmaxf(bm, vm);
+            if (vm > a.m) score_raise(a, vm, c);
+            score_add<V>(r, a.m, c, score_rho(a.m, c), a.s, a.u);
+            if (RANK && vm >= xt) {
+                typename V::Count cnt;
+                V::below(cnt, r, w < vt ? V::pivot(xt) : V::above(xt));
+                n_before += N - V::take(cnt);
+            }
+        }
+        if (TOP) top(bm);
     }
     // the entries outside the vectors
     const u32 loose = cta == 0 ? lead + behind : 0;
@@ -317,13 +403,13 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
         const float e = score_f32(x[j]);
         if (e > a.m) score_raise(a, e, c);
-        const float y = (e - a.m) * c, w = exp2_hw(y);
+        const float y = fmaf(e - a.m, c, -score_rho(a.m, c)), w = exp2_hw(y);
         a.s += w;
         a.u = fmaf(w, fmaxf(y, SCORE_LOW2), a.u);
-        if (RANK) n_below += e < xt || (e == xt && (int32_t)j >= t);
+        if (RANK) n_before += e > xt || (e == xt && (int32_t)j < t);
     }
-    if (RANK && tid == 32 && t >= 0 && vt > v0 && vt <= v1 && (u32)t >= lead && (u32)t < lead + n_vec * N)
-        for (u32 j = t; j < lead + vt * N; j++) n_below += score_f32(x[j]) == xt;
+    if (RANK && tid == NT - 1 && t >= (int32_t)lead && vt >= v0 && vt < v1)
+        for (u32 j = lead + vt * N; j < (u32)t; j++) n_before += score_f32(x[j]) == xt;
     // sums of the CTA
     const auto join = [&](ScoreSum& b, u32& nb) {              // over a warp
         float m = b.m;
@@ -335,8 +421,8 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         if (RANK) nb = __reduce_add_sync(0xFFFFFFFFu, nb);
     };
     const bool has = v0 + tid < v1;
-    join(a, n_below);
-    if (lane == 0) { sh.part[wid] = a; sh.below[wid] = n_below; }
+    join(a, n_before);
+    if (lane == 0) { sh.part[wid] = a; sh.before[wid] = n_before; }
     if (TOP) {
         sh.keys[tid] = has ? (u64)score_order(most1) << 32 | (u32)~first : 0;
         sh.first[tid] = first;
@@ -346,26 +432,27 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     __syncthreads();
     if (wid == NT / 32 - 1) {
         a = lane < NT / 32 ? sh.part[lane] : ScoreSum{SCORE_NONE, 0.0f, 0.0f};
-        n_below = lane < NT / 32 ? sh.below[lane] : 0;
-        join(a, n_below);
-        if (lane == 0) { sh.sum = a; sh.n_below = n_below; }
+        n_before = lane < NT / 32 ? sh.before[lane] : 0;
+        join(a, n_before);
+        if (lane == 0) { sh.sum = a; sh.n_before = n_before; }
     }
     if (TOP) {
-        // the groups' largest values in order: threads 4 i to 4 i + 3 look for the place of group i's
-        if (tid < SCORE_GROUPS) {
+        // the groups' largest values in order
+        if (tid < GROUPS) {
             u64 head = 0;
 #pragma unroll
-            for (int q = 0; q < NT / SCORE_GROUPS; q++) head = max(head, sh.keys[tid + q * SCORE_GROUPS]);
+            for (int q = 0; q < NT / GROUPS; q++) head = max(head, sh.keys[tid + q * GROUPS]);
             sh.heads[tid] = head;
         }
         __syncthreads();
         {
-            const u64 head = sh.heads[tid / 4];
+            constexpr int S = NT / GROUPS;                     // threads that look for the place of a group's
+            const u64 head = sh.heads[tid / S];
             u32 before = 0;
 #pragma unroll
-            for (int o = 0; o < SCORE_GROUPS / 4; o++) before += sh.heads[tid % 4 + 4 * o] > head;
-            before += __shfl_xor_sync(0xFFFFFFFFu, before, 1);
-            before += __shfl_xor_sync(0xFFFFFFFFu, before, 2);
+            for (int o = 0; o < GROUPS / S; o++) before += sh.heads[tid % S + S * o] > head;
+#pragma unroll
+            for (int o = 1; o < S; o <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, o);
             if (head && before == P.top_k - 1) sh.bound = score_key(score_unorder((u32)(head >> 32)), lead + ~(u32)head * N + N - 1);
         }
         __syncthreads();
@@ -373,6 +460,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             const u64 bound = sh.bound;
             const u32 bv = (u32)(bound >> 32), bj = ~(u32)bound;
             const auto look = [&](const uint4& r, u32 w) {
+                if (score_order(V::value(V::most(r))) < bv) return;
 #pragma unroll
                 for (int e = 0; e < N; e++) {
                     const u64 key = score_key(V::at(r, e), lead + w * N + e);
@@ -383,13 +471,9 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             const bool hot = has && (bound == 0 || ov > bv || (ov == bv && lead + first * N <= bj));
             // others of this thread's batches: all of them, or, where only entries equal to the bound's are left, those in front of it
             if (hot && (bound == 0 || (score_order(most2) >= bv && (ov > bv || lead + (b0 + U * NT) * N <= bj)))) sh.scan[atomicAdd(&sh.n_scan, 1u)] = tid;
-            if (hot) {
-                uint4 r[U];
+            uint4 r[U];                                        // (on its way while the list becomes complete and is worked off)
 #pragma unroll
-                for (int i = 0; i < U; i++) r[i] = b0 + tid + i * NT < v1 ? __ldg(vec + b0 + tid + i * NT) : V::lowest();
-#pragma unroll
-                for (int i = 0; i < U; i++) if (b0 + tid + i * NT < v1) look(r[i], b0 + tid + i * NT);
-            }
+            for (int i = 0; i < U; i++) r[i] = hot && b0 + tid + i * NT < v1 ? __ldg(vec + b0 + tid + i * NT) : V::lowest();
             if ((u32)tid < loose) {
                 const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
                 const u64 key = score_key(score_f32(x[j]), j);
@@ -399,11 +483,21 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             const u32 n_scan = sh.n_scan;
             for (u32 i = wid; i < n_scan; i += NT / 32) {
                 const u32 o = sh.scan[i], skip = (sh.first[o] - v0 - o) / (U * NT);
-                for (u32 n = lane; (u64)v0 + o + (u64)n * NT < v1; n += 32) if (n / U != skip) look(__ldg(vec + v0 + o + n * NT), v0 + o + n * NT);
+                for (u64 n0 = lane; v0 + o + n0 * NT < v1; n0 += 32 * U) {
+                    uint4 q[U];
+#pragma unroll
+                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; q[k] = w < v1 ? __ldg(vec + w) : V::lowest(); }
+#pragma unroll
+                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; if (w < v1 && (n0 + 32 * k) / U != skip) look(q[k], (u32)w); }
+                }
+            }
+            if (hot) {
+#pragma unroll
+                for (int i = 0; i < U; i++) if (b0 + tid + i * NT < v1) look(r[i], b0 + tid + i * NT);
             }
             __syncthreads();
             const u32 n_cand = sh.n_cand;
-            score_rank(sh.cand, min(n_cand, (u32)SCORE_CAND), sh.best, P.top_k);
+            score_rank<NT>(sh.cand, min(n_cand, (u32)SCORE_CAND), sh.best, P.top_k);
             __syncthreads();
             if (n_cand <= SCORE_CAND) break;
             if (tid == 0) { sh.bound = sh.best[P.top_k - 1]; sh.n_cand = 0; sh.n_scan = 0; }
@@ -412,31 +506,31 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     } else __syncthreads();
     // the row's from its CTAs'
     ScoreSum sum = sh.sum;
-    n_below = sh.n_below;
+    n_before = sh.n_before;
     if (ctas > 1) {
         cluster_wait();
         if (tid == 0) {
             const u32 at = cluster_map(&sh.all_sum[cta], 0);
             cluster_put(at, sum.m); cluster_put(at + 4, sum.s); cluster_put(at + 8, sum.u);
-            cluster_put(cluster_map(&sh.all_below[cta], 0), __uint_as_float(n_below));
+            cluster_put(cluster_map(&sh.all_before[cta], 0), __uint_as_float(n_before));
         }
         if (TOP && (u32)tid < P.top_k) cluster_put(cluster_map(&sh.all_best[cta * P.top_k + tid], 0), sh.best[tid]);
         cluster_arrive();
         cluster_wait();
         if (cta != 0) return;
         sum = (u32)lane < ctas ? sh.all_sum[lane] : ScoreSum{SCORE_NONE, 0.0f, 0.0f};
-        n_below = (u32)lane < ctas ? sh.all_below[lane] : 0;
-        join(sum, n_below);
-        if (TOP) { score_rank(sh.all_best, ctas * P.top_k, sh.best, P.top_k); __syncthreads(); }
+        n_before = (u32)lane < ctas ? sh.all_before[lane] : 0;
+        join(sum, n_before);
+        if (TOP) { score_rank<NT>(sh.all_best, ctas * P.top_k, sh.best, P.top_k); __syncthreads(); }
     }
     const bool bad = sum.s != sum.s, nothing = sum.s == 0.0f;
-    const float ls = logf(sum.s);
+    const float ln = logf(sum.s), ls = fmaf(score_rho(sum.m, c), 0.6931471806f, ln);       // ls: relative to m itself
     const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : P.scale * (e - sum.m) - ls; };
     if (tid == 0) {
         P.logprob[row] = t < 0 ? 0.0f : log_p(xt);
         if (P.lse) P.lse[row] = bad ? sum.s : nothing ? -INFINITY : fmaf(P.scale, sum.m, ls);
-        if (P.entropy) P.entropy[row] = bad ? sum.s : nothing ? 0.0f : ls - 0.6931471806f * (sum.u / sum.s);
-        if (RANK) P.rank[row] = t < 0 || bad ? 0 : (int32_t)(P.n_vocab - n_below + 1);
+        if (P.entropy) P.entropy[row] = bad ? sum.s : nothing ? 0.0f : ln - 0.6931471806f * (sum.u / sum.s);
+        if (RANK) P.rank[row] = t < 0 || bad ? 0 : (int32_t)(n_before + 1);
     }
     if (TOP && (u32)tid < P.top_k) {
         const u64 key = sh.best[tid];
@@ -485,14 +579,15 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
     typedef ScoreVec<T> V;
     constexpr int N = V::N, U = SCORE_U, NT = SCORE_GRAD_NT;
     cudaGridDependencySynchronize();
-    const unsigned long long row = blockIdx.x / P.parts;
-    const u32 part = blockIdx.x % P.parts, tid = threadIdx.x;
-    if (row == P.n_rows) { score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
+    const unsigned long long row = (blockIdx.x - 1) / P.parts;
+    const u32 part = (blockIdx.x - 1) % P.parts, tid = threadIdx.x;
+    if (blockIdx.x == 0) { score_check<NT>(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, P.status_out); return; }
     const T* x = reinterpret_cast<const T*>(P.logits) + row * P.stride;
     T* dx = reinterpret_cast<T*>(P.grad) + row * P.grad_stride;
     ScoreGradRow R;
     bool in_use;
-    R.t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, in_use);
+    float unused;
+    R.t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, (const T*)nullptr, in_use, unused);
     if (!in_use) return;
     const float g = R.t < 0 ? 0.0f : P.g[row], h = ENT ? P.h[row] : 0.0f;
     R.lse = P.lse[row];
