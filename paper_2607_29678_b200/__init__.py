@@ -367,39 +367,50 @@ class Session:
 # -- around the model: scores of ids, block tables -------------------------------------------------------------------
 
 
-def _dev(t, dtype, name, numel=None, device=None):
-    """Device address of a contiguous CUDA tensor of this type (and size, on this device); raises ValueError otherwise."""
-    if t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} CUDA tensor is needed")
+def _dev(t, dtype, name, numel, index):
+    """Device address of a contiguous tensor of this type (and size) on CUDA device `index`; raises ValueError otherwise."""
+    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor on cuda:{index} is needed, not {t.dtype} on {t.device}")
     if numel is not None and t.numel() != numel:
         raise ValueError(f"{name}: {numel} entries are needed, {t.numel()} given")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name}: on {t.device}, other arguments on {device}")
     return t.data_ptr()
 
 
-def _on(device, stream, call):
-    """call(stream address) with `device` current, on `stream` (a stream of that device) or that device's current stream."""
-    import torch
-    if stream is not None and stream.device != device:
-        raise ValueError(f"stream of {stream.device}, tensors on {device}")
-    if device.index == torch.cuda.current_device():
-        return call(_stream_ptr(stream))
-    with torch.cuda.device(device):
-        return call(_stream_ptr(stream))
+def _opt(bufs, key, dtype, numel, index):
+    t = bufs.get(key)
+    return None if t is None else _dev(t, dtype, key, numel, index)
 
 
-def _logits(logits, name="logits"):
-    """(type code, rows, entries of a row, distance of rows) of a 2-D CUDA tensor whose entries of a row are neighbours."""
+def _call(name, index, stream, before, behind):
+    """The entry point with device `index` current, on `stream` (one of that device) or that device's current stream."""
     import torch
-    kinds = {torch.bfloat16: TT_BF16, torch.float16: TT_FP16, torch.float32: TT_FP32}
-    if logits.dtype not in kinds or not logits.is_cuda or logits.dim() != 2:
+    if index < 0:
+        raise ValueError("CUDA tensors are needed")
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"stream of {stream.device}, tensors on cuda:{index}")
+    f = getattr(_lib or lib(), name)
+    if index == torch._C._cuda_getDevice():
+        # (the address alone: torch.cuda.current_stream() makes an object for it, a microsecond of every call)
+        rc = f(*before, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream, *behind)
+    else:
+        with torch.cuda.device(index):
+            rc = f(*before, _stream_ptr(stream), *behind)
+    if rc != TT_OK:
+        raise TokTierError(rc, name)
+
+
+def _logits(t, name="logits"):
+    """(type code, rows, entries of a row, distance of rows) of a 2-D tensor whose entries of a row are neighbours."""
+    import torch
+    dtype = t.dtype
+    kind = TT_BF16 if dtype is torch.bfloat16 else TT_FP16 if dtype is torch.float16 else TT_FP32 if dtype is torch.float32 else None
+    if kind is None or t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{name}: a 2-D bfloat16, float16 or float32 CUDA tensor is needed")
-    rows, n = logits.shape
-    step, one = logits.stride()
-    if n > 1 and one != 1:
+    rows, n = t.shape
+    step, one = t.stride()
+    if one != 1 and n > 1:
         raise ValueError(f"{name}: the entries of a row have to be neighbours")
-    return kinds[logits.dtype], rows, n, max(step, n) if rows <= 1 else step
+    return kind, rows, n, max(step, n) if rows <= 1 else step
 
 
 def alloc_logprobs(n_rows: int, top_k: int = 0, device="cuda") -> dict:
@@ -419,41 +430,37 @@ def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None):
     [n_rows], ids_off = int64 CUDA tensor [n_docs + 1] (as encode_batch leaves it) or None.  Results land in bufs as alloc_logprobs makes them; 'logprob'
     and 'status' have to be there, the others are left out where they are missing; the second size of 'top_ids' is top_k."""
     import torch
+    i32, f32 = torch.int32, torch.float32
     kind, rows, n, step = _logits(logits)
-    dev = logits.device
-
-    def out(name, dtype, numel=rows):
-        t = bufs.get(name)
-        return None if t is None else _dev(t, dtype, name, numel, dev)
-
+    dev = logits.get_device()
     top = bufs.get("top_ids")
     if (top is None) != (bufs.get("top_logprobs") is None) or (top is not None and (top.dim() != 2 or top.shape[0] != rows)):
         raise ValueError("top_ids and top_logprobs: both [n_rows, top_k], or neither")
     k = 0 if top is None else top.shape[1]
-    args = (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
-            None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1, k)
-    outs = (_dev(bufs["logprob"], torch.float32, "logprob", rows, dev), out("lse", torch.float32), out("entropy", torch.float32),
-            out("rank", torch.int32), out("top_ids", torch.int32, rows * k) if k else None, out("top_logprobs", torch.float32, rows * k) if k else None,
-            _dev(bufs["status"], torch.int32, "status", 1, dev))
-    _check(_on(dev, stream, lambda st: lib().tt_logprobs(*args, st, *outs)), "tt_logprobs")
+    _call("tt_logprobs", dev, stream,
+          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, i32, "ids", rows, dev),
+           None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1, k),
+          (_dev(bufs["logprob"], f32, "logprob", rows, dev), _opt(bufs, "lse", f32, rows, dev), _opt(bufs, "entropy", f32, rows, dev),
+           _opt(bufs, "rank", i32, rows, dev), _dev(top, i32, "top_ids", rows * k, dev) if k else None,
+           _dev(bufs["top_logprobs"], f32, "top_logprobs", rows * k, dev) if k else None, _dev(bufs["status"], i32, "status", 1, dev)))
 
 
 def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entropy=None, scale: float = 1.0, stream=None):
     """tt_logprobs_grad: bufs as logprobs() left them for the same logits, ids, ids_off and scale ('lse', with grad_entropy also 'entropy';
     'status' is written again).  grad_logprob / grad_entropy: float32 CUDA tensors [n_rows]; grad: like logits, or logits itself."""
     import torch
+    f32 = torch.float32
     kind, rows, n, step = _logits(logits)
-    dev = logits.device
+    dev = logits.get_device()
     gkind, grows, gn, gstep = _logits(grad, "grad")
-    if (gkind, grows, gn) != (kind, rows, n) or grad.device != dev:
+    if gkind != kind or grows != rows or gn != n or grad.get_device() != dev:
         raise ValueError("grad: of the type, size and device of logits")
-    args = (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
-            None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1,
-            _dev(bufs["lse"], torch.float32, "lse", rows, dev), None if grad_entropy is None else _dev(bufs["entropy"], torch.float32, "entropy", rows, dev),
-            _dev(grad_logprob, torch.float32, "grad_logprob", rows, dev),
-            None if grad_entropy is None else _dev(grad_entropy, torch.float32, "grad_entropy", rows, dev))
-    status = _dev(bufs["status"], torch.int32, "status", 1, dev)
-    _check(_on(dev, stream, lambda st: lib().tt_logprobs_grad(*args, st, grad.data_ptr(), gstep, status)), "tt_logprobs_grad")
+    _call("tt_logprobs_grad", dev, stream,
+          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
+           None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1,
+           _dev(bufs["lse"], f32, "lse", rows, dev), None if grad_entropy is None else _dev(bufs["entropy"], f32, "entropy", rows, dev),
+           _dev(grad_logprob, f32, "grad_logprob", rows, dev), None if grad_entropy is None else _dev(grad_entropy, f32, "grad_entropy", rows, dev)),
+          (grad.data_ptr(), gstep, _dev(bufs["status"], torch.int32, "status", 1, dev)))
 
 
 def alloc_blocks(n_req: int, table_width: int, n_blocks: int, max_tokens: int, device="cuda"):
@@ -472,17 +479,20 @@ def alloc_blocks(n_req: int, table_width: int, n_blocks: int, max_tokens: int, d
 def _blocks(state, bufs, block_size):
     """The arguments that both calls share: (device, requests, those before the stream, those behind it)."""
     import torch
+    i32, i64 = torch.int32, torch.int64
     table, free = state["block_table"], state["free_blocks"]
     if table.dim() != 2:
         raise ValueError("block_table: [n_req, table_width] is needed")
-    n, dev = table.shape[0], table.device
     if block_size <= 0:
         raise ValueError("block_size: at least 1")
-    ws = bufs["workspace"]
-    before = (_dev(state["seq_len"], torch.int32, "seq_len", n, dev), block_size, _dev(table, torch.int32, "block_table"), table.shape[1],
-              _dev(free, torch.int32, "free_blocks", None, dev), free.numel(), _dev(state["n_free"], torch.int64, "n_free", 1, dev))
-    behind = (_dev(bufs["seq_len"], torch.int32, "seq_len", n, dev), _dev(bufs["n_free"], torch.int64, "n_free", 1, dev),
-              _dev(bufs["status"], torch.int32, "status", 1, dev), _dev(ws, torch.uint8, "workspace", None, dev), ws.numel())
+    n, width = table.shape
+    dev, ws = table.get_device(), bufs["workspace"]
+    if dev < 0:
+        raise ValueError("CUDA tensors are needed")
+    before = (_dev(state["seq_len"], i32, "seq_len", n, dev), block_size, _dev(table, i32, "block_table", None, dev), width,
+              _dev(free, i32, "free_blocks", None, dev), free.numel(), _dev(state["n_free"], i64, "n_free", 1, dev))
+    behind = (_dev(bufs["seq_len"], i32, "seq_len", n, dev), _dev(bufs["n_free"], i64, "n_free", 1, dev),
+              _dev(bufs["status"], i32, "status", 1, dev), _dev(ws, torch.uint8, "workspace", None, dev), ws.numel())
     return dev, n, before, behind
 
 
@@ -493,18 +503,15 @@ def blocks_extend(new_off, state, block_size: int, bufs, stream=None):
     dev, n, before, behind = _blocks(state, bufs, block_size)
     slots = bufs["slots"]
     cap = slots.numel()
-    maps = [None if bufs.get(k) is None else _dev(bufs[k], torch.int32, k, cap, dev) for k in ("positions", "requests")]
-    off = _dev(new_off, torch.int64, "new_off", n + 1, dev)
-    sp = _dev(slots, torch.int64, "slots", None, dev)
-    _check(_on(dev, stream, lambda st: lib().tt_blocks_extend(off, n, *before, st, sp, cap, *maps, *behind)), "tt_blocks_extend")
+    _call("tt_blocks_extend", dev, stream, (_dev(new_off, torch.int64, "new_off", n + 1, dev), n, *before),
+          (_dev(slots, torch.int64, "slots", None, dev), cap, _opt(bufs, "positions", torch.int32, cap, dev), _opt(bufs, "requests", torch.int32, cap, dev), *behind))
 
 
 def blocks_release(keep_len, state, block_size: int, bufs, stream=None):
     """tt_blocks_release: keep_len = int32 CUDA tensor [n_req], tokens that each request keeps; state and bufs as for blocks_extend."""
     import torch
     dev, n, before, behind = _blocks(state, bufs, block_size)
-    keep = _dev(keep_len, torch.int32, "keep_len", n, dev)
-    _check(_on(dev, stream, lambda st: lib().tt_blocks_release(keep, n, *before, st, *behind)), "tt_blocks_release")
+    _call("tt_blocks_release", dev, stream, (_dev(keep_len, torch.int32, "keep_len", n, dev), n, *before), behind)
 
 
 class VerifierStats(ctypes.Structure):

@@ -13,10 +13,28 @@ static int blocks_args(BlocksParams& P, size_t n_req, const int32_t* seq_len, si
     if (!n_free || !n_free_out || !status_out || !workspace || (n_req && (!seq_len || !seq_out || (width && !table))) || (free_cap && !free_blocks)) return TT_ERR_ARG;
     if (((uintptr_t)workspace & 255) != 0 || workspace_bytes < tt_blocks_workspace_bytes(n_req)) return TT_ERR_ARG;
     P = BlocksParams{};
+    unsigned sh = 0;
+    while ((size_t)1 << sh < block_size) sh++;
+    P.div_shift = 31 + sh; P.div_mul = (u32)((((size_t)1 << (31 + sh)) + block_size - 1) / block_size);
     P.seq_len = seq_len; P.n_req = (u32)n_req; P.block = (u32)block_size; P.width = (u32)width; P.table = const_cast<int32_t*>(table);
     P.free_blocks = const_cast<int32_t*>(free_blocks); P.free_cap = free_cap; P.n_free = (const long long*)n_free;
     P.seq_out = seq_out; P.n_free_out = (long long*)n_free_out; P.status_out = status_out;
     P.plan = (BlocksPlan*)workspace; P.per = (int2*)((char*)workspace + blocks_up(sizeof(BlocksPlan)));
+    return TT_OK;
+}
+
+// `most`: entries (tokens, blocks) that the call may have to write.  Up to BLOCKS_FEW requests and 16 entries a thread of the cluster: one kernel.
+template <bool EXTEND>
+static int blocks_launch(const BlocksParams& P, size_t most, cudaStream_t st) {
+    if (P.n_req <= BLOCKS_FEW && most <= (size_t)16 * BLOCKS_CLUSTER * BLOCKS_THREADS) {
+        const unsigned ctas = most <= 2 * BLOCKS_THREADS ? 1 : BLOCKS_CLUSTER;
+        TT_TRY(host_launch(k_blocks_few<EXTEND>, ctas, BLOCKS_THREADS, ctas, 0, st, P));
+        return TT_OK;
+    }
+    const int sms = host_sm_count();
+    if (!sms) return TT_ERR_CUDA;
+    TT_TRY(host_launch(k_blocks_plan<EXTEND>, 1, BLOCKS_THREADS, 1, 0, st, P));
+    if (P.n_req) TT_TRY(host_launch(EXTEND ? k_blocks_extend : k_blocks_release, (unsigned)sms * BLOCKS_WRITE_CTAS, BLOCKS_WRITE_NT, 1, 0, st, P));
     return TT_OK;
 }
 
@@ -29,11 +47,7 @@ extern "C" int tt_blocks_extend(const int64_t* new_off, size_t n_req, const int3
     if (rc != TT_OK) return rc;
     if ((n_req && !new_off) || slots_cap >= ((size_t)1 << 31) || (slots_cap && !slots_out)) return TT_ERR_ARG;
     P.new_off = (const long long*)new_off; P.slots = (long long*)slots_out; P.slots_cap = slots_cap; P.pos = pos_out; P.req = req_out;
-    const int sms = host_sm_count();
-    if (!sms) return TT_ERR_CUDA;
-    TT_TRY(host_launch(k_blocks_plan<true>, 1, BLOCKS_THREADS, 1, 0, (cudaStream_t)stream, P));
-    if (n_req) TT_TRY(host_launch(k_blocks_extend, (unsigned)sms * 8, 256, 1, 0, (cudaStream_t)stream, P));
-    return TT_OK;
+    return blocks_launch<true>(P, slots_cap, (cudaStream_t)stream);
 }
 
 extern "C" int tt_blocks_release(const int32_t* keep_len, size_t n_req, const int32_t* seq_len, size_t block_size, const int32_t* block_table, size_t table_width,
@@ -44,9 +58,6 @@ extern "C" int tt_blocks_release(const int32_t* keep_len, size_t n_req, const in
     if (rc != TT_OK) return rc;
     if (n_req && !keep_len) return TT_ERR_ARG;
     P.keep = keep_len;
-    const int sms = host_sm_count();
-    if (!sms) return TT_ERR_CUDA;
-    TT_TRY(host_launch(k_blocks_plan<false>, 1, BLOCKS_THREADS, 1, 0, (cudaStream_t)stream, P));
-    if (n_req) TT_TRY(host_launch(k_blocks_release, (unsigned)sms * 8, 256, 1, 0, (cudaStream_t)stream, P));
-    return TT_OK;
+    const size_t most = (size_t)n_req * table_width;
+    return blocks_launch<false>(P, most < free_cap ? most : free_cap, (cudaStream_t)stream);
 }

@@ -473,7 +473,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             if (hot && (bound == 0 || (score_order(most2) >= bv && (ov > bv || lead + (b0 + U * NT) * N <= bj)))) sh.scan[atomicAdd(&sh.n_scan, 1u)] = tid;
             uint4 r[U];                                        // (on its way while the list becomes complete and is worked off)
 #pragma unroll
-            for (int i = 0; i < U; i++) r[i] = hot && b0 + tid + i * NT < v1 ? __ldg(vec + b0 + tid + i * NT) : V::lowest();
+            for (int i = 0; i < U; i++) r[i] = hot && b0 + tid + i * NT < v1 ? __ldcg(vec + b0 + tid + i * NT) : V::lowest();
             if ((u32)tid < loose) {
                 const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
                 const u64 key = score_key(score_f32(x[j]), j);
@@ -486,7 +486,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
                 for (u64 n0 = lane; v0 + o + n0 * NT < v1; n0 += 32 * U) {
                     uint4 q[U];
 #pragma unroll
-                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; q[k] = w < v1 ? __ldg(vec + w) : V::lowest(); }
+                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; q[k] = w < v1 ? __ldcg(vec + w) : V::lowest(); }
 #pragma unroll
                     for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; if (w < v1 && (n0 + 32 * k) / U != skip) look(q[k], (u32)w); }
                 }
@@ -589,9 +589,9 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
     float unused;
     R.t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, (const T*)nullptr, in_use, unused);
     if (!in_use) return;
-    const float g = R.t < 0 ? 0.0f : P.g[row], h = ENT ? P.h[row] : 0.0f;
-    R.lse = P.lse[row];
-    R.scale = P.scale; R.A = -P.scale * (ENT ? fmaf(h, P.entropy[row], g) : g); R.B = -P.scale * h; R.hot = P.scale * g;
+    const float g = R.t < 0 ? 0.0f : __ldcg(P.g + row), h = ENT ? __ldcg(P.h + row) : 0.0f;
+    R.lse = __ldcg(P.lse + row);
+    R.scale = P.scale; R.A = -P.scale * (ENT ? fmaf(h, __ldcg(P.entropy + row), g) : g); R.B = -P.scale * h; R.hot = P.scale * g;
     const bool zeros = (g == 0.0f && h == 0.0f) || R.lse == -INFINITY;
     // 16-byte vectors where rows of both lie alike in memory; else the logits are read entry by entry
     const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)dx & 15)) & 15) / (u32)sizeof(T));
