@@ -150,6 +150,9 @@ template <> struct ScoreVec<float> {
     __device__ static Most larger(Most a, Most b) { return fmaxf(a, b); }
     __device__ static float value(Most m) { return m; }
     __device__ static uint4 lowest() { const u32 w = 0xFF800000u; return make_uint4(w, w, w, w); }
+    static constexpr float LOW = -1e37f;                       // stands for lower values and -inf, see `masked`
+    __device__ static u32 raised(u32 w) { return __float_as_uint(__uint_as_float(w) < LOW ? LOW : __uint_as_float(w)); }
+    __device__ static uint4 raised(const uint4& r) { return make_uint4(raised(r.x), raised(r.y), raised(r.z), raised(r.w)); }
     __device__ static Pivot pivot(float x) { return x; }
     // the next larger value
     __device__ static Pivot above(float x) {
@@ -164,7 +167,7 @@ template <> struct ScoreVec<float> {
 };
 // The 16-bit types: a word is two values; counts are sums of 1.0 in the type itself, exact up to 256.
 template <typename T2> __device__ __forceinline__ T2 as_two(u32 w) { T2 v; memcpy(&v, &w, 4); return v; }
-template <typename T, typename T2, u32 LOWEST> struct ScoreVec16 {
+template <typename T, typename T2, u32 LOWEST, u32 LOWER> struct ScoreVec16 {         // bits of -inf, and of what stands for it
     static constexpr int N = 8;
     typedef T2 Pivot;
     struct Count { T2 n = as_two<T2>(0); };
@@ -174,6 +177,8 @@ template <typename T, typename T2, u32 LOWEST> struct ScoreVec16 {
     __device__ static Most larger(Most a, Most b) { return __hmax2(a, b); }
     __device__ static float value(Most m) { return fmaxf(score_f32(m.x), score_f32(m.y)); }
     __device__ static uint4 lowest() { const u32 w = LOWEST << 16 | LOWEST; return make_uint4(w, w, w, w); }
+    __device__ static u32 raised(u32 w) { const T2 v = __hmax2_nan(as_two<T2>(w), as_two<T2>(LOWER << 16 | LOWER)); u32 o; memcpy(&o, &v, 4); return o; }
+    __device__ static uint4 raised(const uint4& r) { return make_uint4(raised(r.x), raised(r.y), raised(r.z), raised(r.w)); }
     __device__ static Pivot bits_pivot(u32 h) { return as_two<T2>(h << 16 | h); }
     __device__ static void below(Count& c, const uint4& r, Pivot p) {
 #pragma unroll
@@ -182,14 +187,16 @@ template <typename T, typename T2, u32 LOWEST> struct ScoreVec16 {
     __device__ static u32 take(Count& c) { const u32 n = (u32)(score_f32(c.n.x) + score_f32(c.n.y)); c.n = as_two<T2>(0); return n; }
     __device__ static u32 next_bits(u32 b) { return (b & 0x7FFF) == 0 ? 1u : b & 0x8000 ? b - 1 : b + 1; }
 };
-template <> struct ScoreVec<__nv_bfloat16> : ScoreVec16<__nv_bfloat16, __nv_bfloat162, 0xFF80u> {
+template <> struct ScoreVec<__nv_bfloat16> : ScoreVec16<__nv_bfloat16, __nv_bfloat162, 0xFF80u, 0xFCF0u> {
+    static constexpr float LOW = -9.969209968386869e36f;       // 0xFCF0
     __device__ static float at(const uint4& r, int e) { const u32 w = word(r, e >> 1); return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16); }
     __device__ static f32x2 pair(const uint4& r, int p) { const u32 w = word(r, p); return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
     __device__ static u32 bits(float x) { return __float_as_uint(x) >> 16; }
     __device__ static Pivot pivot(float x) { return bits_pivot(bits(x)); }
     __device__ static Pivot above(float x) { return bits_pivot(next_bits(bits(x))); }
 };
-template <> struct ScoreVec<__half> : ScoreVec16<__half, __half2, 0xFC00u> {
+template <> struct ScoreVec<__half> : ScoreVec16<__half, __half2, 0xFC00u, 0xFBFFu> {
+    static constexpr float LOW = -65504.0f;
     __device__ static float at(const uint4& r, int e) { const __half2 h = as_two<__half2>(word(r, e >> 1)); return __half2float(e & 1 ? h.y : h.x); }
     __device__ static f32x2 pair(const uint4& r, int p) { const float2 f = __half22float2(as_two<__half2>(word(r, p))); return pair_of(f.x, f.y); }
     __device__ static u32 bits(float x) { return __half_as_ushort(__float2half_rn(x)); }
@@ -331,6 +338,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         return up;
     };
     u32 stage = 0, v = v0 + tid;
+    bool masked = false;                                       // a batch held masked logits
     for (; (u64)v + (U - 1) * NT < v1; v += U * NT, stage ^= 1) {
         copy_wait<1>();
         uint4 r[U];
@@ -346,6 +354,12 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             for (int i = U - 2; i >= 0; i--) if (V::value(vm[i]) == bm) first = v + i * NT;
         }
         if (bm > a.m) { score_raise(a, bm, c); ref = score_ref(bm, c); }
+        // From then on a low number stands for -inf, whose terms are 0 without a NaN: where the largest logit is far above it, so that its terms are 0,
+        // too, and the id's is above it, so that the count below is the same.
+        if (masked && (V::LOW - a.m) * c < SCORE_LOW && xt > V::LOW) {
+#pragma unroll
+            for (int i = 0; i < U; i++) r[i] = V::raised(r[i]);
+        }
         const f32x2 ref2 = pair_of(-ref, -ref);
         f32x2 s2 = pair_of(0.0f, 0.0f), u2 = s2;
 #pragma unroll
@@ -364,6 +378,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         pair_to(s2, s0, s1); pair_to(u2, u0, u1);
         s0 += s1; u0 += u1;
         if (u0 != u0) {                                        // masked logits, or some beyond the range of a product
+            masked = true;
             s0 = u0 = 0.0f;
             const float rho = score_rho(a.m, c);
 #pragma unroll

@@ -291,6 +291,28 @@ def test_scores_of_masked_and_broken_rows(tt, kind, n):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,n", [(6, 20_001), (160, 9_000), (900, 4_100)])
+def test_masks_through_long_rows(tt, kind, rows, n):
+    """Masked entries in every batch of a thread, of either kind and mixed, with the row's id masked, low or the only one left."""
+    import torch
+    low, inf = torch.finfo(_kind(kind)).min, float("inf")
+    x = make_logits(kind, rows, n, seed=rows)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    gone = torch.rand((rows, n), generator=g, device="cuda")
+    x.masked_fill_(gone < 0.4, -inf)
+    x[::2].masked_fill_(gone[::2] > 0.7, low)
+    x[1::6, n // 2:] = low
+    x[4::12] -= 30_000.0
+    x[5::12] = torch.where(gone[5::12] < 0.5, torch.tensor(low, dtype=x.dtype, device="cuda"), torch.tensor(low, dtype=x.dtype, device="cuda") * 0.99)
+    x[3::18] = -inf; x[3::18, n - 7] = 2.0
+    x[7::20] = low; x[7::20, ::3] = -inf
+    ids = make_ids(rows, n, rows)
+    bufs, _ = run_scores(tt, x, ids, 5, scale=1.25 if kind == "fp16" else 1.0)
+    check_scores(x, ids, bufs, scale=1.25 if kind == "fp16" else 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("n", [257, 8_200, 50_001, 150_000])
 def test_alternatives_where_the_largest_lie_together(tt, kind, n):
     """Sorted rows, plateaus of equal values, large values at regular distances: whatever the shares that threads take of a row."""
