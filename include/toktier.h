@@ -188,8 +188,8 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
  *   scale       > 0 and at most 2^100 (1 / temperature).
  *   ids         DEVICE int32[n_rows].  ids_off = NULL: row i is asked for ids[i]; a negative id asks for nothing.
  *   ids_off     DEVICE int64[n_docs + 1] as tt_encode_batch leaves it, or NULL (then n_docs is 0): row i is what the model said behind
- *               token i, and is asked for ids[i + 1] if that token is of the same document, else for nothing.  Rows from
- *               ids_off[n_docs] on are not read and nothing of theirs is written.
+ *               token i, and is asked for ids[i + 1] if that token is of the same document, else for nothing.  Nothing is
+ *               written of the rows from ids_off[n_docs] on (their logits may be read).
  *   logprob_out, lse_out, entropy_out  DEVICE float[n_rows]; rank_out DEVICE int32[n_rows]; any but logprob_out may be NULL.
  *   top_ids_out, top_logprob_out       DEVICE int32 / float [n_rows][top_k], top_k <= TT_TOP_MAX and <= n_vocab; top_k = 0: both NULL.
  *   status_out  DEVICE int32: TT_OK; TT_ERR_CAPACITY if ids_off[n_docs] > n_rows (nothing else is written); else TT_ERR_ARG if ids_off does not

@@ -79,6 +79,7 @@ extern "C" int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, si
     const size_t batch = (size_t)SCORE_GRAD_NT * SCORE_U * 16, bytes = n_vocab * score_size(dtype), places = (size_t)sms * 5 * 4;
     size_t rounds = 4;
     while (rounds > 1 && n_rows * ((bytes + rounds * batch - 1) / (rounds * batch)) < places) rounds /= 2;
+    if (n_rows * ((bytes + rounds * batch - 1) / (rounds * batch)) >= (size_t)0x7FFFFFFF) return TT_ERR_ARG;
     P.rounds = (u32)rounds; P.parts = (u32)((bytes + rounds * batch - 1) / (rounds * batch));
     TT_TRY(dtype == TT_BF16 ? launch_logprobs_grad<__nv_bfloat16>(P, (cudaStream_t)stream) : dtype == TT_FP16 ? launch_logprobs_grad<__half>(P, (cudaStream_t)stream)
                             : launch_logprobs_grad<float>(P, (cudaStream_t)stream));

@@ -41,6 +41,8 @@ struct ScoreGradParams {
 __device__ __forceinline__ float score_f32(float x) { return x; }
 __device__ __forceinline__ float score_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float score_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+// A logit, past L1: a CTA may be placed while the kernel that wrote it still runs on the same SM.
+template <typename T> __device__ __forceinline__ float score_ld(const T* p) { return score_f32(__ldcg(p)); }
 __device__ __forceinline__ void score_put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void score_put(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void score_put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
@@ -106,7 +108,7 @@ __device__ __forceinline__ int32_t score_target(const int32_t* ids, unsigned lon
     const bool shifted = off != nullptr;
     int32_t id = !shifted || i + 1 < n_rows ? __ldcg(ids + i + shifted) : -1;
     if (id < 0 || (u32)id >= n_vocab) id = -1;
-    xt = x && id >= 0 ? score_f32(x[id]) : INFINITY;
+    xt = x && id >= 0 ? score_ld(x + id) : INFINITY;
     in_use = true;
     if (shifted) {
         const long long total = __ldcg(off + n_docs);
@@ -213,12 +215,12 @@ __device__ __forceinline__ float score_unorder(u32 o) { return __uint_as_float(o
 __device__ __forceinline__ u64 score_key(float x, u32 j) { return (u64)score_order(x) << 32 | (u32)~j; }
 
 // Largest logit m seen and, relative to it and in powers of two, the sums: s of 2^y, u of y 2^y with y = x c - M, c = scale / ln 2, M = m c
-// rounded, which is one multiply-add for each logit and pair of sums.  What the rounding of M leaves, rho = M - m c, takes part in every step
-// from one m to another, so that nothing is lost by it.  Where m c is too large for that (a row of the type's lowest value), M is a NaN and rho 0: the sums of such a batch are
+// rounded: one multiply-add a logit.  What the rounding of M leaves, rho = M - m c, takes part in every step from one m to another and in the end, so
+// that nothing is lost by it.  Where m c is too large for that (2^20: rho stays below 2^-4), M is a NaN and rho 0: the sums of such a batch are
 // NaNs, and it is worked out again as y = (x - m) c - rho, as are batches with a y of -inf (masked logits), whose product with 2^y is a NaN.
 // m starts at the lowest number, so that rows of -inf leave s = 0 and no difference of infinities arises.
 struct ScoreSum { float m, s, u; };
-constexpr float SCORE_NONE = -3.402823466e38f, SCORE_LARGE = 1e30f;
+constexpr float SCORE_NONE = -3.402823466e38f, SCORE_LARGE = 1048576.0f;
 __device__ __forceinline__ float score_ref(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? M : NAN; }
 __device__ __forceinline__ float score_rho(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? -fmaf(m, c, -M) : 0.0f; }
 __device__ __forceinline__ void score_raise(ScoreSum& a, float m, float c) {      // to a reference m >= a.m
@@ -239,13 +241,15 @@ __device__ __forceinline__ void score_add(const uint4& r, float m, float c, floa
     }
 }
 
-// A row goes to a cluster of CTAs, a stretch of its 16-byte vectors to each; thread i of a CTA takes every SCORE_NT-th of them from the i-th
-// on, SCORE_U at a time (a batch); SCORE_PLACES threads of 80 registers are on an SM at once (with 64, 1,024 of them,
-// the loop spills: 4,096 rows of 100,256 16-bit logits with alternatives 252 us, so 176).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives
-// each thread also keeps the largest value among its vectors, the first vector that has it, and the largest value of its other batches.  The
-// top_k-th of the largest values of 64 groups of threads, with the end of its vector, is a bound that at least top_k entries reach; what reaches
-// it is then looked up again: in the one batch of each thread whose largest value does, and in the whole share of the few threads with a second
-// batch that does.
+// A row goes to a cluster of CTAs, a stretch of its 16-byte vectors to each; thread i of a CTA takes every NT-th of them from the i-th on, SCORE_U
+// at a time (a batch).  One pass over the row keeps the sums and counts what lies before the row's id.  For the alternatives each thread also
+// keeps the largest value among its vectors, the first vector that has it, and the largest value of its other batches.  The top_k-th of the largest
+// values of 64 groups of threads, with the end of its vector, is a bound that at least top_k entries reach; what reaches it is then looked up
+// again: in the one batch of each thread whose largest value does, and in the whole share of the few threads with a second batch that does.
+//   Bound by the bytes of the logits while the clock is high: 4,015 rows of 200,000 bf16 252 us, 6.4 TB/s (98 % of a copy's rate).  A long run of such
+// calls meets the power limit; at 1.6 GHz the exponentials (16 a clock and SM: 212 us) and the rest of the arithmetic bound it, 305 us.
+//   SCORE_PLACES threads of 80 registers are on an SM at once: with 64 registers, for 1,024 threads, the loop spills (4,096 rows of 100,256 bf16 logits
+// with twenty alternatives 252 us, so 173).
 constexpr int SCORE_U = 4, SCORE_CAND = 512, SCORE_CLUSTER = 8, SCORE_PLACES = 768;
 
 template <int SCORE_NT>
@@ -289,7 +293,7 @@ template <typename T, bool TOP, bool RANK, int NT>
 __global__ void __launch_bounds__(NT, SCORE_PLACES / NT)
 k_logprobs(const __grid_constant__ ScoreParams P) {
     typedef ScoreVec<T> V;
-    constexpr int N = V::N, U = SCORE_U, GROUPS = NT < 64 ? NT : 64;
+    constexpr int N = V::N, U = SCORE_U, GROUPS = 64;
     __shared__ ScoreShared<NT> sh;
     __shared__ uint4 ring[2][U][NT];
     const u32 ctas = 1u << P.log_ctas, cta = blockIdx.x & (ctas - 1);
@@ -310,25 +314,35 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     const u32 v0 = (u32)((u64)n_vec * cta >> P.log_ctas), v1 = (u32)((u64)n_vec * (cta + 1) >> P.log_ctas);
     // Two batches are on their way to the thread's own places in shared memory, so that the loads of one run under the arithmetic of the other (and
     // the first two while the row's id is looked up).
-    const auto fetch = [&](u32 stage, u64 v) {
+    const auto fetch = [&](u32 stage, u32 v) {                  // (fewer than 2^29 vectors: no sum passes 32 bits)
+        if (v + (U - 1) * NT < v1) {
 #pragma unroll
-        for (int i = 0; i < U; i++) if (v + i * NT < v1) copy_async(&ring[stage][i][tid], vec + v + i * NT);
+            for (int i = 0; i < U; i++) copy_async(&ring[stage][i][tid], vec + v + i * NT);
+        } else {
+#pragma unroll
+            for (int i = 0; i < U; i++) if (v + i * NT < v1) copy_async(&ring[stage][i][tid], vec + v + i * NT);
+        }
         copy_commit();
     };
     fetch(0, v0 + tid);
-    fetch(1, (u64)v0 + tid + U * NT);
+    fetch(1, v0 + tid + U * NT);
     bool in_use;
     float xt;
     const int32_t t = score_target(P.ids, P.n_rows, P.n_vocab, P.ids_off, P.n_docs, row, x, in_use, xt);
-    if (!in_use) { if (ctas > 1) cluster_wait(); return; }
+    if (!in_use) { copy_wait<0>(); if (ctas > 1) cluster_wait(); return; }
     const float c = P.scale2;
     const f32x2 c2 = pair_of(c, c);
-    // entries before the row's id: those not below it in the vectors in front of the id's, those not below the next larger value in the others;
-    // equal ones in front of it in its own vector are added at the end
+    // entries before the row's id: those not below it in the vectors in front of the id's, those not below the next larger value in the others, and
+    // the equal ones in front of it in its own vector, which one thread counts here (by one load: entry by entry past L1 it took 2 us)
     const u32 vt = t < (int32_t)lead ? 0 : min(n_vec, ((u32)t - lead) / N);
     ScoreSum a = {SCORE_NONE, 0.0f, 0.0f};
     float ref = NAN;
     u32 n_before = 0;
+    if (RANK && tid == NT - 1 && t >= (int32_t)lead && vt >= v0 && vt < v1) {
+        const uint4 w = __ldcg(vec + vt);
+#pragma unroll
+        for (int e = 0; e < N; e++) n_before += lead + vt * N + e < (u32)t && V::at(w, e) == xt;
+    }
     float most1 = -INFINITY, most2 = -INFINITY;
     u32 first = v0 + tid;                                      // (of a thread that has vectors; none of -inf alone is passed over)
     const auto top = [&](float bm) {                           // a batch's largest value: does it raise the thread's?
@@ -339,7 +353,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     };
     u32 stage = 0, v = v0 + tid;
     bool masked = false;                                       // a batch held masked logits
-    for (; (u64)v + (U - 1) * NT < v1; v += U * NT, stage ^= 1) {
+    for (; v + (U - 1) * NT < v1; v += U * NT, stage ^= 1) {
         copy_wait<1>();
         uint4 r[U];
         typename V::Most vm[U], h;
@@ -347,15 +361,15 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         for (int i = 0; i < U; i++) { r[i] = ring[stage][i][tid]; vm[i] = V::most(r[i]); h = i ? V::larger(h, vm[i]) : vm[i]; }
         const float bm = V::value(h);
         asm volatile("" :: "f"(bm) : "memory");                // (all of the batch is in registers: its place is free)
-        fetch(stage, (u64)v + 2 * U * NT);
+        fetch(stage, v + 2 * U * NT);
         if (TOP && top(bm)) {
             first = v + (U - 1) * NT;
 #pragma unroll
             for (int i = U - 2; i >= 0; i--) if (V::value(vm[i]) == bm) first = v + i * NT;
         }
         if (bm > a.m) { score_raise(a, bm, c); ref = score_ref(bm, c); }
-        // From then on a low number stands for -inf, whose terms are 0 without a NaN: where the largest logit is far above it, so that its terms are 0,
-        // too, and the id's is above it, so that the count below is the same.
+        // Once a thread has met masked logits a low number stands for -inf, whose terms are 0 without a NaN: where the largest logit is far above it, so
+        // that its terms are 0, too, and the id's is above it, so that the count below is the same.
         if (masked && (V::LOW - a.m) * c < SCORE_LOW && xt > V::LOW) {
 #pragma unroll
             for (int i = 0; i < U; i++) r[i] = V::raised(r[i]);
@@ -416,15 +430,13 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     const u32 loose = cta == 0 ? lead + behind : 0;
     if ((u32)tid < loose) {
         const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
-        const float e = score_f32(x[j]);
+        const float e = score_ld(x + j);
         if (e > a.m) score_raise(a, e, c);
         const float y = fmaf(e - a.m, c, -score_rho(a.m, c)), w = exp2_hw(y);
         a.s += w;
         a.u = fmaf(w, fmaxf(y, SCORE_LOW2), a.u);
         if (RANK) n_before += e > xt || (e == xt && (int32_t)j < t);
     }
-    if (RANK && tid == NT - 1 && t >= (int32_t)lead && vt >= v0 && vt < v1)
-        for (u32 j = lead + vt * N; j < (u32)t; j++) n_before += score_f32(x[j]) == xt;
     // sums of the CTA
     const auto join = [&](ScoreSum& b, u32& nb) {              // over a warp
         float m = b.m;
@@ -471,7 +483,8 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             if (head && before == P.top_k - 1) sh.bound = score_key(score_unorder((u32)(head >> 32)), lead + ~(u32)head * N + N - 1);
         }
         __syncthreads();
-        while (sh.sum.s == sh.sum.s) {                         // (not where there is a NaN; again where more entries reach the bound than there is room for: each time with a bound that fewer reach)
+        // (not where there is a NaN; again where more entries reach the bound than there is room for: each time with a bound that fewer reach)
+        while (sh.sum.s == sh.sum.s) {
             const u64 bound = sh.bound;
             const u32 bv = (u32)(bound >> 32), bj = ~(u32)bound;
             const auto look = [&](const uint4& r, u32 w) {
@@ -491,19 +504,19 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
             for (int i = 0; i < U; i++) r[i] = hot && b0 + tid + i * NT < v1 ? __ldcg(vec + b0 + tid + i * NT) : V::lowest();
             if ((u32)tid < loose) {
                 const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
-                const u64 key = score_key(score_f32(x[j]), j);
+                const u64 key = score_key(score_ld(x + j), j);
                 if (key >= bound) { const u32 n = atomicAdd(&sh.n_cand, 1u); if (n < SCORE_CAND) sh.cand[n] = key; }
             }
             __syncthreads();
             const u32 n_scan = sh.n_scan;
             for (u32 i = wid; i < n_scan; i += NT / 32) {
                 const u32 o = sh.scan[i], skip = (sh.first[o] - v0 - o) / (U * NT);
-                for (u64 n0 = lane; v0 + o + n0 * NT < v1; n0 += 32 * U) {
+                for (u32 n0 = lane; v0 + o + n0 * NT < v1; n0 += 32 * U) {
                     uint4 q[U];
 #pragma unroll
-                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; q[k] = w < v1 ? __ldcg(vec + w) : V::lowest(); }
+                    for (int k = 0; k < U; k++) { const u32 w = v0 + o + (n0 + 32 * k) * NT; q[k] = w < v1 ? __ldcg(vec + w) : V::lowest(); }
 #pragma unroll
-                    for (int k = 0; k < U; k++) { const u64 w = v0 + o + (n0 + 32 * k) * NT; if (w < v1 && (n0 + 32 * k) / U != skip) look(q[k], (u32)w); }
+                    for (int k = 0; k < U; k++) { const u32 w = v0 + o + (n0 + 32 * k) * NT; if (w < v1 && (n0 + 32 * k) / U != skip) look(q[k], w); }
                 }
             }
             if (hot) {
@@ -540,11 +553,12 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     }
     const bool bad = sum.s != sum.s, nothing = sum.s == 0.0f;
     const float ln = logf(sum.s), ls = fmaf(score_rho(sum.m, c), 0.6931471806f, ln);       // ls: relative to m itself
-    const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : P.scale * (e - sum.m) - ls; };
+    // (what rounding leaves of a probability of 1 is not above it, and no entropy is below 0)
+    const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : fminf(P.scale * (e - sum.m) - ls, 0.0f); };
     if (tid == 0) {
         P.logprob[row] = t < 0 ? 0.0f : log_p(xt);
         if (P.lse) P.lse[row] = bad ? sum.s : nothing ? -INFINITY : fmaf(P.scale, sum.m, ls);
-        if (P.entropy) P.entropy[row] = bad ? sum.s : nothing ? 0.0f : ln - 0.6931471806f * (sum.u / sum.s);
+        if (P.entropy) P.entropy[row] = bad ? sum.s : nothing ? 0.0f : fmaxf(ln - 0.6931471806f * (sum.u / sum.s), 0.0f);
         if (RANK) P.rank[row] = t < 0 || bad ? 0 : (int32_t)(n_before + 1);
     }
     if (TOP && (u32)tid < P.top_k) {
@@ -555,7 +569,8 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
 }
 
 // The gradient: with L = scale x_j - lse,  dx_j = exp(L) (A + B L) + [j = t] scale g,  A = -scale (g + h entropy), B = -scale h.
-// Reads a row once and writes it once; a CTA takes a stretch of SCORE_GRAD_NT * SCORE_U * rounds vectors of a row.
+// Reads a row once and writes it once; a CTA takes a stretch of SCORE_GRAD_NT * SCORE_U * rounds vectors of a row.  Bound by those bytes: 4,015 rows
+// of 200,000 bf16 logits 477 us, 6.7 TB/s (104 % of a copy's rate); in a long run of calls, at the power limit, 515.
 constexpr int SCORE_GRAD_NT = 256;
 
 struct ScoreGradRow { float scale, lse, A, B, hot; int32_t t; };
@@ -620,7 +635,7 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
         const T* e = x + lead + (size_t)v * N;
         uint4 r; T w[N];
 #pragma unroll
-        for (int i = 0; i < N; i++) w[i] = e[i];
+        for (int i = 0; i < N; i++) w[i] = __ldcg(e + i);
         memcpy(&r, w, 16);
         return r;
     };
@@ -658,6 +673,6 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
     const u32 loose = lead + (P.n_vocab - lead - n_vec * N);
     if (part == 0 && tid < loose) {
         const u32 j = tid < lead ? tid : n_vec * N + tid;
-        score_put(dx + j, zeros ? 0.0f : score_grad_one<ENT>(R, score_f32(x[j]), j));
+        score_put(dx + j, zeros ? 0.0f : score_grad_one<ENT>(R, score_ld(x + j), j));
     }
 }

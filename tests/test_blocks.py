@@ -309,3 +309,85 @@ def test_decode_steps_replayed_from_a_graph(tt):
     for step in range(40):
         graphs[step % 2].replay()
         agree(pool, state, bufs, pool.extend(np.arange(n + 1)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,share", [(30_000, 0.02), (9_000, 0.3), (2_500, 0.001), (100_000, 0.0005)])
+def test_most_requests_get_nothing(tt, n, share):
+    """Thousands of requests without a new token between those with some, and of requests that give no block back."""
+    import torch
+    rng = np.random.default_rng(n)
+    old = rng.integers(0, 40, n)
+    new = np.where(rng.random(n) < share, rng.integers(1, 120, n), 0)
+    new[n // 2] = 3_000
+    off = np.r_[0, np.cumsum(new)]
+    need = int((-(-(old + new) // 16) - (-(-old // 16))).sum())
+    pool, state = setup(n, 16, old, need, 200, n)
+    bufs = buffers(tt, state, int(off[-1]), True)
+    maps = pool.extend(off)
+    tt.blocks_extend(cuda(off, torch.int64), state, 16, bufs)
+    agree(pool, state, bufs, maps)
+    keep = np.where(rng.random(n) < 0.9, pool.seq, pool.seq // 2)
+    pool.release(keep)
+    tt.blocks_release(cuda(keep, torch.int32), state, 16, bufs)
+    agree(pool, state, bufs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,most", [(40, 30), (5, 60_000), (3_000, 90)])
+def test_maps_at_odd_addresses(tt, n, most):
+    import torch
+    rng = np.random.default_rng(n)
+    old, new = rng.integers(0, 50, n), rng.integers(0, most, n)
+    off = np.r_[0, np.cumsum(new)]
+    need = int((-(-(old + new) // 16) - (-(-old // 16))).sum())
+    width = int((-(-(old + new) // 16)).max()) + 1
+    total = int(off[-1])
+    for shift in (1, 2, 3):
+        pool, state = setup(n, 16, old, need, width, n)
+        whole = {"slots": torch.full((total + 8,), -5, dtype=torch.int64, device="cuda"), "positions": torch.full((total + 8,), -5, dtype=torch.int32, device="cuda"),
+                 "requests": torch.full((total + 8,), -5, dtype=torch.int32, device="cuda")}
+        bufs = dict(buffers(tt, state, total, False), **{k: v[shift:shift + total] for k, v in whole.items()})
+        maps = pool.extend(off)
+        tt.blocks_extend(cuda(off, torch.int64), state, 16, bufs)
+        agree(pool, state, bufs, maps)
+        for v in whole.values():
+            assert (v[:shift] == -5).all() and (v[shift + total:] == -5).all()
+
+
+@pytest.mark.gpu
+def test_two_pools_on_two_streams(tt):
+    """Calls on different pools and workspaces do not meet; large ones captured, with both directions in one graph."""
+    import torch
+    pools, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for k in range(2):
+        rng = np.random.default_rng(k)
+        n = 3_000 + k
+        old, new = rng.integers(0, 60, n), rng.integers(0, 90, n)
+        off = np.r_[0, np.cumsum(new)]
+        pool, state = setup(n, 16, old, 40_000, 16, k)
+        pools.append((pool, state, buffers(tt, state, int(off[-1]), True), off, cuda(off, torch.int64), cuda(old, torch.int32), old))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for st, (pool, state, bufs, off, d_off, d_old, old) in zip(streams, pools):
+            with torch.cuda.stream(st):
+                tt.blocks_extend(d_off, state, 16, bufs)
+                tt.blocks_release(d_old, state, 16, bufs)
+    torch.cuda.synchronize()
+    for pool, state, bufs, off, d_off, d_old, old in pools:
+        maps = pool.extend(off)
+        pool.release(old)
+        agree(pool, state, bufs, maps)
+    pool, state, bufs, off, d_off, d_old, old = pools[0]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        tt.blocks_extend(d_off, state, 16, bufs)
+        tt.blocks_release(d_old, state, 16, bufs)
+        tt.blocks_extend(d_off, state, 16, bufs)
+        tt.blocks_release(d_old, state, 16, bufs)
+    bufs["slots"].fill_(-5)
+    graph.replay()
+    torch.cuda.synchronize()
+    want = Pool(pool.table, pool.seq, pool.free, pool.n_free, 16)
+    slots, _, _ = want.extend(off)
+    assert np.array_equal(bufs["slots"].cpu().numpy(), slots) and np.array_equal(state["seq_len"].cpu().numpy(), old) and int(state["n_free"].item()) == pool.n_free

@@ -562,3 +562,105 @@ def test_binding_refuses_on_a_device(tt):
         tt.logprobs(x[:1].expand(4, 50), ids, bufs)                        # rows that lie over one another
     with pytest.raises(tt.TokTierError):
         tt.logprobs(x, ids, bufs, scale=0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,rows,n,k", [("bf16", 200, 50_001, 7), ("fp32", 200, 50_001, 3), ("fp16", 1_000, 10_001, 2), ("bf16", 1_300, 9_003, 0), ("fp32", 460, 4_096, 32), ("bf16", 500, 700, 1), ("fp16", 1_500, 3_001, 4)])
+def test_every_way_a_row_is_shared_out(tt, kind, rows, n, k):
+    """Rows by the hundred and thousand: CTAs of 64, 128 and 256 threads, alone and in clusters."""
+    x = make_logits(kind, rows, n, seed=n)
+    ids = make_ids(rows, n, n, none_every=7)
+    bufs, _ = run_scores(tt, x, ids, k)
+    check_scores(x, ids, bufs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_subnormal_logits_keep_their_order(tt, kind):
+    import torch
+    n = 2_100
+    least = {"bf16": 2.0 ** -133, "fp16": 2.0 ** -24, "fp32": 2.0 ** -149}[kind]
+    g = torch.Generator().manual_seed(3)
+    x = (torch.randint(-120, 121, (4, n), generator=g).double() * least).to(_kind(kind)).cuda()
+    x[3] = 0.0; x[3, 5] = -least; x[3, 7] = least; x[3, 9] = -0.0
+    ids = make_ids(4, n, 3)
+    ids[3] = 9
+    bufs, _ = run_scores(tt, x, ids, 32)
+    check_scores(x, ids, bufs)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [3, 700, 33_000])
+def test_sure_rows_stay_within_their_range(tt, kind, n):
+    """One entry with all of the probability: no logprob above 0, no entropy below."""
+    import torch
+    x = torch.full((64, n), -float("inf"), dtype=_kind(kind), device="cuda")
+    ids = make_ids(64, n, 1)
+    at = torch.arange(64, device="cuda")
+    x[at, ids.long()] = (torch.randn(64, generator=torch.Generator(device="cuda").manual_seed(n), device="cuda") * 25).to(_kind(kind))
+    x[32:] = torch.where(torch.isinf(x[32:]), x[32:].amax(1, keepdim=True) - 30, x[32:])
+    for scale in (1.0, 0.37, 4.0):
+        bufs, _ = run_scores(tt, x, ids, 2, scale=scale)
+        check_scores(x, ids, bufs, scale=scale)
+        assert float(bufs["logprob"].max()) <= 0.0 and float(bufs["top_logprobs"].max()) <= 0.0 and float(bufs["entropy"].min()) >= 0.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("scale", [2.0 ** 100, 1e6, 300.0, 1e-3, 1e-30, 1e-42])
+@pytest.mark.parametrize("kind", KINDS)
+def test_extreme_scales(tt, kind, scale):
+    x = make_logits(kind, 5, 4_001, seed=2)
+    x[1, ::3] = -float("inf")
+    ids = make_ids(5, 4_001, 4)
+    bufs, _ = run_scores(tt, x, ids, 5, scale=scale)
+    if scale > 1e5:                                                        # lse and log probabilities of that size: their leading digits
+        del bufs["lse"]
+    check_scores(x, ids, bufs, scale=scale)
+
+
+@pytest.mark.gpu
+def test_thousands_of_documents(tt):
+    """Three steps of the search for a row's document; documents without a token between the others."""
+    import torch
+    rng = np.random.default_rng(5)
+    lengths = rng.integers(0, 4, 5_000)
+    lengths[rng.integers(0, 5_000, 1_500)] = 0
+    off = np.r_[0, np.cumsum(lengths)].astype(np.int64)
+    rows, n = int(off[-1]) + 3, 64
+    x, ids = make_logits("bf16", rows, n, seed=1), make_ids(rows, n, 1)
+    toff = torch.from_numpy(off).cuda()
+    bufs, before = run_scores(tt, x, ids, 0, ids_off=toff)
+    check_scores(x, ids, bufs, ids_off=toff, untouched=before)
+    starts = set(off.tolist())
+    wrong = ids.clone()
+    wrong[[i for i in range(rows - 3) if i in starts]] = n + 7             # asked for by no row
+    run_scores(tt, x, wrong, 0, ids_off=toff)
+    inner = next(i for i in range(2_000, rows - 3) if i not in starts)
+    wrong[inner] = n
+    run_scores(tt, x, wrong, 0, ids_off=toff, status=tt.TT_ERR_BAD_IDS)
+
+
+@pytest.mark.gpu
+def test_two_calls_at_once(tt):
+    """Nothing is shared between calls: the same buffers read on two streams, each with outputs of its own."""
+    import torch
+    x, y = make_logits("fp16", 700, 9_001, seed=1), make_logits("fp16", 700, 9_001, seed=2)
+    ids = make_ids(700, 9_001, 1)
+    want = [run_scores(tt, v, ids, 8)[0] for v in (x, y)]
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [tt.alloc_logprobs(700, 8), tt.alloc_logprobs(700, 8)]
+    g = torch.randn(700, device="cuda")
+    grads = [torch.zeros_like(x), torch.zeros_like(y)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, v, b, d in zip(streams, (x, y), got, grads):
+            with torch.cuda.stream(st):
+                tt.logprobs(v, ids, b)
+                tt.logprobs_grad(v, ids, b, g, d)
+    torch.cuda.synchronize()
+    for w, b, v, d in zip(want, got, (x, y), grads):
+        for k in w:
+            assert torch.equal(w[k], b[k]), k
+        alone = torch.zeros_like(d)
+        tt.logprobs_grad(v, ids, w, g, alone)
+        assert torch.equal(alone, d)
