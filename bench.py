@@ -614,12 +614,13 @@ def vocab_table_bytes(n_merges: int) -> int:
 
 
 def csrc_hash() -> str:
-    """SHA-256 over the CUDA sources (the figures below belong to one state of them)."""
+    """SHA-256 over the CUDA sources of the tokenizer (the figures below belong to one state of them); the kernels around the model
+    are compiled apart from it."""
     import hashlib
     h = hashlib.sha256()
     d = os.path.join(ROOT, "paper_2607_29678_b200", "csrc")
     for f in sorted(os.listdir(d)):
-        if f.endswith((".cu", ".cuh", ".inc")):
+        if f.endswith((".cu", ".cuh", ".inc")) and not f.startswith(("tt_scores", "tt_blocks", "tt_host")):
             with open(os.path.join(d, f), "rb") as fh:
                 h.update(f.encode()); h.update(fh.read())
     return h.hexdigest()[:16]
