@@ -21,16 +21,21 @@ static cudaError_t launch_logprobs_nt(const ScoreParams& P, cudaStream_t st) {
 }
 // Threads of a CTA and CTAs of a row.  An SM has places for SCORE_PLACES threads.
 //   Short rows, many of them: CTAs of 64 (4,096 rows of 8.7 KB: 64 threads 17 us, with alternatives 32, 128 threads 23 and 38, 256 39 and 59).
-//   Otherwise 128 threads where the rows alone fill the GPU (4,096 rows of 200 KB: 64 threads 139 us, 128 133, 256 141; with alternatives 218,
-//   169, 182), but for a second round that would be less than half full, which 64 threads avoid (1,000 rows of 400 KB: 66, 90, 74).
-//   Fewer rows: up to one for each SM 256 threads, else 128, and a cluster for a row as long as its CTAs have places and 48 KB each
-//   (one row of 200 KB: 1 CTA 11.6 us, 4 7.7; 64 rows of 400 KB: 1 CTA 21, 4 14.9, 8 24; 300 of 400 KB: 42, of 2 CTAs 36, 4 37, 8 46;
-//   64 rows of 64 KB: 1 CTA 8.8, 2 9.2, 8 15.7).
+//   Up to one row for each SM 256 threads, otherwise 128 (4,096 rows of 200 KB: 64 threads 139 us, 128 133, 256 141; with alternatives 218, 169, 182).
+//   But between half a round and one and a half of CTAs of 128 threads, where the SMs get one or two more or less: long 16-bit rows, bound by arithmetic
+//   too, take 256 (1,024 rows of 400 KB: 64 threads 86 us, 128 85, 256 73; with alternatives 124, 100, 93), others behind a full round 64, all at
+//   once (1,000 rows of 400 KB in 32 bits: 66, 90, 74; 1,100 of 64 KB: 27, 28, 30).
+//   Fewer rows: a cluster for a row as long as its CTAs have places and 48 KB each (one row of 200 KB: 1 CTA 11.6 us, 4 7.7; 64 rows of 400 KB:
+//   1 CTA 21, 4 14.9, 8 24; 300 of 400 KB: 42, of 2 CTAs 36, 4 37, 8 46; 64 rows of 64 KB: 1 CTA 8.8, 2 9.2, 8 15.7).
 template <typename T>
 static cudaError_t launch_logprobs(ScoreParams& P, size_t sms, cudaStream_t st) {
-    const size_t bytes = (size_t)P.n_vocab * sizeof(T), places = sms * SCORE_PLACES;
+    const size_t bytes = (size_t)P.n_vocab * sizeof(T), places = sms * SCORE_PLACES, half = places / 256, full = places / 128;
     P.log_ctas = 0;
-    if ((bytes <= 16384 && P.n_rows > places / 256) || (P.n_rows > places / 128 && P.n_rows <= places / 128 * 3 / 2)) return launch_logprobs_nt<T, 64>(P, st);
+    if (P.n_rows > half && bytes <= 16384) return launch_logprobs_nt<T, 64>(P, st);
+    if (P.n_rows > half && P.n_rows <= full * 3 / 2) {
+        if (sizeof(T) == 2 && bytes >= 131072) return launch_logprobs_nt<T, 256>(P, st);
+        if (P.n_rows > full) return launch_logprobs_nt<T, 64>(P, st);
+    }
     const size_t nt = P.n_rows <= sms ? 256 : 128;
     while (2u << P.log_ctas <= SCORE_CLUSTER && (P.n_rows * nt << (P.log_ctas + 1)) <= places && bytes >> (P.log_ctas + 1) >= 49152) P.log_ctas++;
     return nt == 256 ? launch_logprobs_nt<T, 256>(P, st) : launch_logprobs_nt<T, 128>(P, st);

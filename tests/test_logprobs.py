@@ -565,7 +565,8 @@ def test_binding_refuses_on_a_device(tt):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("kind,rows,n,k", [("bf16", 200, 50_001, 7), ("fp32", 200, 50_001, 3), ("fp16", 1_000, 10_001, 2), ("bf16", 1_300, 9_003, 0), ("fp32", 460, 4_096, 32), ("bf16", 500, 700, 1), ("fp16", 1_500, 3_001, 4)])
+@pytest.mark.parametrize("kind,rows,n,k", [("bf16", 200, 50_001, 7), ("fp32", 200, 50_001, 3), ("fp16", 1_000, 10_001, 2), ("bf16", 1_300, 9_003, 0), ("fp32", 460, 4_096, 32), ("bf16", 500, 700, 1), ("fp16", 1_500, 3_001, 4),
+                                            ("bf16", 460, 65_601, 20)])
 def test_every_way_a_row_is_shared_out(tt, kind, rows, n, k):
     """Rows by the hundred and thousand: CTAs of 64, 128 and 256 threads, alone and in clusters."""
     x = make_logits(kind, rows, n, seed=n)
