@@ -80,7 +80,8 @@ extern "C" int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, si
     P.lse = lse; P.entropy = entropy; P.g = grad_logprob; P.h = grad_entropy; P.grad = grad_out; P.status_out = status_out;
     const int sms = host_sm_count();
     if (!sms) return TT_ERR_CUDA;
-    // a CTA takes up to four batches of 16 KB, fewer where that makes less than four rounds of CTAs (five on an SM)
+    // a CTA takes up to four batches of 16 KB, so that a row's scalars are looked up for more of it, fewer where that makes less than four rounds of CTAs
+    // (five on an SM): 1,000 rows of 64 KB with one batch 24.7 us, with four 25.7
     const size_t batch = (size_t)SCORE_GRAD_NT * SCORE_U * 16, bytes = n_vocab * score_size(dtype), places = (size_t)sms * 5 * 4;
     size_t rounds = 4;
     while (rounds > 1 && n_rows * ((bytes + rounds * batch - 1) / (rounds * batch)) < places) rounds /= 2;
