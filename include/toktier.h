@@ -197,7 +197,9 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
  *               [0, n_vocab) (without ids_off: of n_vocab or more), and is then treated as asked for nothing.
  * A row asked for nothing has logprob 0 and rank 0.  Logits of -inf, or so low that their probability is 0 in 32 bits, count as
  * probability 0.  A row of -inf alone: lse and all ln p are -inf, entropy 0.  A row with a NaN or a +inf: lse, entropy and all ln p are NaN
- * (the logprob of a row asked for nothing stays 0), rank 0, top ids -1.  Sums are held in 32 bits.  The outputs do not overlap the inputs.
+ * (the logprob of a row asked for nothing stays 0), rank 0, top ids -1.  Sums are held in 32 bits.  Where scale times a row's largest logit is beyond
+ * them, its lse is an infinity, of no use for the gradient; the other outputs are not touched by that.  The outputs do not overlap the inputs.  Addresses
+ * are multiples of their type's size.
  *
  * tt_logprobs_grad -- the gradient: given g = dL/dlogprob and h = dL/dentropy of every row (and lse, entropy as tt_logprobs left them for the
  * same logits, ids, offsets and scale),   dL/dx[j] = scale * ( g ([j = t] - p[j]) - h p[j] (ln p[j] + entropy) ),   without the g part where the row is

@@ -11,6 +11,7 @@ static int blocks_args(BlocksParams& P, size_t n_req, const int32_t* seq_len, si
     const size_t most = (size_t)1 << 31;
     if (n_req >= ((size_t)1 << 24) || !block_size || block_size >= most || width >= most || free_cap >= most) return TT_ERR_ARG;
     if (!n_free || !n_free_out || !status_out || !workspace || (n_req && (!seq_len || !seq_out || (width && !table))) || (free_cap && !free_blocks)) return TT_ERR_ARG;
+    if (host_misaligned(4, seq_len, table, free_blocks, seq_out, status_out) || host_misaligned(8, n_free, n_free_out)) return TT_ERR_ARG;
     if (((uintptr_t)workspace & 255) != 0 || workspace_bytes < tt_blocks_workspace_bytes(n_req)) return TT_ERR_ARG;
     P = BlocksParams{};
     unsigned sh = 0;
@@ -48,6 +49,7 @@ extern "C" int tt_blocks_extend(const int64_t* new_off, size_t n_req, const int3
     BlocksParams P;
     const int rc = blocks_args(P, n_req, seq_len, block_size, block_table, table_width, free_blocks, free_cap, n_free, seq_len_out, n_free_out, status_out, workspace, workspace_bytes);
     if (rc != TT_OK) return rc;
+    if (host_misaligned(4, pos_out, req_out) || host_misaligned(8, new_off, slots_out)) return TT_ERR_ARG;
     if ((n_req && !new_off) || slots_cap >= ((size_t)1 << 31) || (slots_cap && !slots_out)) return TT_ERR_ARG;
     P.new_off = (const long long*)new_off; P.slots = (long long*)slots_out; P.slots_cap = slots_cap; P.pos = pos_out; P.req = req_out;
     return blocks_launch<true>(P, slots_cap, (cudaStream_t)stream);
@@ -59,7 +61,7 @@ extern "C" int tt_blocks_release(const int32_t* keep_len, size_t n_req, const in
     BlocksParams P;
     const int rc = blocks_args(P, n_req, seq_len, block_size, block_table, table_width, free_blocks, free_cap, n_free, seq_len_out, n_free_out, status_out, workspace, workspace_bytes);
     if (rc != TT_OK) return rc;
-    if (n_req && !keep_len) return TT_ERR_ARG;
+    if ((n_req && !keep_len) || host_misaligned(4, keep_len)) return TT_ERR_ARG;
     P.keep = keep_len;
     const size_t most = (size_t)n_req * table_width;
     return blocks_launch<false>(P, most < free_cap ? most : free_cap, (cudaStream_t)stream);

@@ -9,6 +9,9 @@ typedef uint64_t u64;
 
 #define TT_TRY(x) do { if ((x) != cudaSuccess) { cudaGetLastError(); return TT_ERR_CUDA; } } while (0)
 
+// Is one of the addresses no multiple of `align` (a power of two)?
+template <typename... P> static inline bool host_misaligned(size_t align, P... p) { return ((((uintptr_t)p) | ...) & (align - 1)) != 0; }
+
 // SMs of the current device, 0 on an error (asked for at every call: an attribute query costs well under a microsecond, and the
 // current device may change between calls).
 static inline int host_sm_count() {

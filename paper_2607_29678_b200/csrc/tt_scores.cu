@@ -9,7 +9,8 @@ static int score_args(const void* logits, int dtype, size_t n_rows, size_t n_voc
                       const int64_t* ids_off, size_t n_docs, const int32_t* status_out) {
     if (dtype != TT_BF16 && dtype != TT_FP16 && dtype != TT_FP32) return TT_ERR_ARG;
     if (!status_out || (n_rows && (!logits || !ids)) || !n_vocab || n_vocab >= ((size_t)1 << 31) || n_rows >= ((size_t)1 << 24)) return TT_ERR_ARG;
-    if (row_stride < n_vocab || row_stride >= ((size_t)1 << 38) || ((uintptr_t)logits & (score_size(dtype) - 1)) != 0) return TT_ERR_ARG;
+    if (row_stride < n_vocab || row_stride >= ((size_t)1 << 38)) return TT_ERR_ARG;
+    if (host_misaligned(score_size(dtype), logits) || host_misaligned(4, ids, status_out) || host_misaligned(8, ids_off)) return TT_ERR_ARG;
     if (!(scale > 0.0f && scale <= 0x1p100f) || (ids_off == nullptr && n_docs != 0) || n_docs >= ((size_t)1 << 31)) return TT_ERR_ARG;
     return TT_OK;
 }
@@ -47,6 +48,7 @@ extern "C" int tt_logprobs(const void* logits, int dtype, size_t n_rows, size_t 
     const int rc = score_args(logits, dtype, n_rows, n_vocab, row_stride, scale, ids, ids_off, n_docs, status_out);
     if (rc != TT_OK) return rc;
     if ((n_rows && !logprob_out) || top_k > TT_TOP_MAX || top_k > n_vocab) return TT_ERR_ARG;
+    if (host_misaligned(4, logprob_out, lse_out, entropy_out, rank_out, top_ids_out, top_logprob_out)) return TT_ERR_ARG;
     if (top_k ? n_rows && (!top_ids_out || !top_logprob_out) : top_ids_out || top_logprob_out) return TT_ERR_ARG;
     ScoreParams P;
     P.logits = logits; P.n_rows = n_rows; P.stride = row_stride; P.n_vocab = (u32)n_vocab; P.top_k = (u32)top_k; P.scale = scale;
@@ -72,7 +74,8 @@ extern "C" int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, si
     const int rc = score_args(logits, dtype, n_rows, n_vocab, row_stride, scale, ids, ids_off, n_docs, status_out);
     if (rc != TT_OK) return rc;
     if ((n_rows && (!lse || !grad_logprob || !grad_out)) || (grad_entropy != nullptr) != (entropy != nullptr)) return TT_ERR_ARG;
-    if (grad_stride < n_vocab || grad_stride >= ((size_t)1 << 38) || ((uintptr_t)grad_out & (score_size(dtype) - 1)) != 0) return TT_ERR_ARG;
+    if (grad_stride < n_vocab || grad_stride >= ((size_t)1 << 38)) return TT_ERR_ARG;
+    if (host_misaligned(score_size(dtype), grad_out) || host_misaligned(4, lse, entropy, grad_logprob, grad_entropy)) return TT_ERR_ARG;
     if (n_rows && grad_out == logits && grad_stride != row_stride) return TT_ERR_ARG;
     ScoreGradParams P;
     P.logits = logits; P.n_rows = n_rows; P.stride = row_stride; P.grad_stride = grad_stride; P.n_vocab = (u32)n_vocab; P.scale = scale;

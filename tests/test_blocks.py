@@ -72,9 +72,10 @@ def test_refusals_without_a_device(tt):
 
     both = [dict(n=1 << 24, ws_bytes=1 << 40), dict(seq=None), dict(block=0), dict(block=1 << 31), dict(table=None), dict(width=1 << 31), dict(free=None), dict(cap=1 << 31), dict(nf=None),
             dict(seq_out=None), dict(nf_out=None), dict(status=None), dict(ws=None), dict(ws=a + 16), dict(ws_bytes=tt.lib().tt_blocks_workspace_bytes(3) - 1)]
-    for kw in both + [dict(off=None), dict(slots=None), dict(scap=1 << 31)]:
+    both += [dict(seq=a + 2), dict(table=a + 1), dict(free=a + 2), dict(nf=a + 4), dict(seq_out=a + 2), dict(nf_out=a + 4), dict(status=a + 2)]
+    for kw in both + [dict(off=None), dict(off=a + 4), dict(slots=None), dict(slots=a + 4), dict(scap=1 << 31)]:
         assert ext(**kw) == tt.TT_ERR_ARG, kw
-    for kw in both + [dict(keep=None)]:
+    for kw in both + [dict(keep=None), dict(keep=a + 2)]:
         assert rel(**kw) == tt.TT_ERR_ARG, kw
     import torch
     with pytest.raises(ValueError):

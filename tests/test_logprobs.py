@@ -183,14 +183,14 @@ def test_refusals_without_a_device(tt):
     bad = [dict(logits=None), dict(logits=a + 1), dict(logits=a + 2, dtype=2), dict(dtype=3), dict(dtype=-1), dict(n=0), dict(n=1 << 31, stride=1 << 31), dict(rows=1 << 24),
            dict(stride=7), dict(stride=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=2.0 ** 101), dict(scale=float("nan")), dict(ids=None), dict(docs=1),
            dict(lp=None), dict(status=None), dict(k=9, top_i=a, top_l=a), dict(k=33, n=64, stride=64, top_i=a, top_l=a), dict(k=1), dict(k=1, top_i=a), dict(top_i=a, top_l=a),
-           dict(off=a, docs=1 << 31)]
+           dict(off=a, docs=1 << 31), dict(off=a + 4, docs=1), dict(ids=a + 2), dict(status=a + 1), dict(lp=a + 2), dict(k=1, top_i=a + 1, top_l=a), dict(k=1, top_i=a, top_l=a + 2)]
     for kw in bad:
         assert fwd(**kw) == tt.TT_ERR_ARG, kw
 
     def bwd(logits=a, rows=2, n=8, stride=8, lse=a, ent=None, g=a, h=None, grad=2 * a, gstride=8, status=a, dtype=0):
         return L.tt_logprobs_grad(logits, dtype, rows, n, stride, 1.0, a, None, 0, lse, ent, g, h, None, grad, gstride, status)
 
-    for kw in [dict(lse=None), dict(g=None), dict(h=a), dict(ent=a), dict(grad=None), dict(gstride=7), dict(grad=a, gstride=9), dict(grad=2 * a + 1), dict(status=None), dict(dtype=5)]:
+    for kw in [dict(lse=None), dict(g=None), dict(h=a), dict(ent=a), dict(grad=None), dict(gstride=7), dict(grad=a, gstride=9), dict(grad=2 * a + 1), dict(lse=a + 2), dict(g=a + 1), dict(h=a + 2, ent=a), dict(h=a, ent=a + 1), dict(status=None), dict(dtype=5)]:
         assert bwd(**kw) == tt.TT_ERR_ARG, kw
 
 
