@@ -35,27 +35,34 @@ struct BlocksParams {
 __device__ __forceinline__ u32 blocks_div(const BlocksParams& P, u32 x) { return (u32)((u64)x * P.div_mul >> P.div_shift); }
 __device__ __forceinline__ u32 blocks_of(const BlocksParams& P, u32 tokens) { const u32 b = blocks_div(P, tokens); return b + (b * P.block != tokens); }
 
-// One request: the change of its blocks and its new length; `bad` collects the status bits (1 argument, 2 capacity).
+// One request's lengths (nothing depends on a load here, so that those of all of a thread's requests are on their way at once), and the change of its
+// blocks and its new length; `bad` collects the status bits (1 argument, 2 capacity).
+struct BlocksLen { int32_t c; long long a, b; };                       // tokens in the cache; extend: offsets of the new ones and behind them; release: a = tokens kept
 template <bool EXTEND>
-__device__ __forceinline__ u32 blocks_change(const BlocksParams& P, u32 r, int32_t& c, int32_t& c_new, u32& bad) {
-    c = __ldcg(P.seq_len + r);
-    c_new = c;
-    if (c < 0) { bad |= 1; return 0; }
+__device__ __forceinline__ BlocksLen blocks_len(const BlocksParams& P, u32 r) {
+    BlocksLen l;
+    l.c = __ldcg(P.seq_len + r);
+    l.a = EXTEND ? __ldcg(P.new_off + r) : __ldcg(P.keep + r);
+    l.b = EXTEND ? __ldcg(P.new_off + r + 1) : 0;
+    return l;
+}
+template <bool EXTEND>
+__device__ __forceinline__ u32 blocks_change(const BlocksParams& P, u32 r, const BlocksLen& l, int32_t& c_new, u32& bad) {
+    c_new = l.c;
+    if (l.c < 0) { bad |= 1; return 0; }
     if constexpr (EXTEND) {
-        const long long a = __ldcg(P.new_off + r), b = __ldcg(P.new_off + r + 1);
-        if (b < a || a < 0 || (r == 0 && a != 0)) { bad |= 1; return 0; }
-        if (b - a > (long long)0x7FFFFFFF - c) { bad |= 2; return 0; }
-        c_new = c + (int32_t)(b - a);
-        const u32 have = blocks_of(P, (u32)c), want = blocks_of(P, (u32)c_new);
+        if (l.b < l.a || l.a < 0 || (r == 0 && l.a != 0)) { bad |= 1; return 0; }
+        if (l.b - l.a > (long long)0x7FFFFFFF - l.c) { bad |= 2; return 0; }
+        c_new = l.c + (int32_t)(l.b - l.a);
+        const u32 have = blocks_of(P, (u32)l.c), want = blocks_of(P, (u32)c_new);
         if (want > P.width) { bad |= 2; return 0; }
         return want - have;
     } else {
-        const int32_t k = __ldcg(P.keep + r);
-        if (k < 0 || k > c) { bad |= 1; return 0; }
-        c_new = k;
-        const u32 have = blocks_of(P, (u32)c);
+        if (l.a < 0 || l.a > l.c) { bad |= 1; return 0; }
+        c_new = (int32_t)l.a;
+        const u32 have = blocks_of(P, (u32)l.c);
         if (have > P.width) { bad |= 2; return 0; }
-        return have - blocks_of(P, (u32)k);
+        return have - blocks_of(P, (u32)l.a);
     }
 }
 
@@ -77,12 +84,11 @@ __device__ __forceinline__ long long blocks_scan(long long x, long long* buf, lo
 }
 
 // What the lengths alone do not say: the free list's count, room for the tokens; then the sum of the changes against the list.
-template <bool EXTEND>
-__device__ __forceinline__ u32 blocks_bad(const BlocksParams& P, long long n_free) {
-    u32 bad = n_free < 0 || (unsigned long long)n_free > P.free_cap ? 1 : 0;
-    if (EXTEND && P.n_req) { const long long t = __ldcg(P.new_off + P.n_req); if (t > 0 && (unsigned long long)t > P.slots_cap) bad |= 2; }
-    return bad;
+__device__ __forceinline__ u32 blocks_bad(const BlocksParams& P, long long n_free, long long tokens) {
+    return (n_free < 0 || (unsigned long long)n_free > P.free_cap ? 1 : 0) | (tokens > 0 && (unsigned long long)tokens > P.slots_cap ? 2 : 0);
 }
+template <bool EXTEND>
+__device__ __forceinline__ long long blocks_tokens(const BlocksParams& P) { return EXTEND && P.n_req ? __ldcg(P.new_off + P.n_req) : 0; }
 template <bool EXTEND>
 __device__ __forceinline__ int blocks_status(const BlocksParams& P, u32 bad, long long n_free, long long total) {
     if (total > (EXTEND ? n_free : (long long)P.free_cap - n_free)) bad |= 2;
@@ -102,32 +108,34 @@ k_blocks_few(const __grid_constant__ BlocksParams P) {
     __shared__ long long s_scan[32];
     const u32 ctas = gridDim.x, cta = blockIdx.x, tid = threadIdx.x;
     cudaGridDependencySynchronize();
-    const long long n_free = __ldcg(P.n_free);
-    u32 bad = blocks_bad<EXTEND>(P, n_free);
-    int32_t c[2] = {0, 0}, c_new[2] = {0, 0};
+    const long long n_free = __ldcg(P.n_free), all = blocks_tokens<EXTEND>(P);
+    BlocksLen l[2] = {};
+    int32_t c_new[2] = {0, 0};
     u32 change[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; i++) if (2 * tid + i < P.n_req) l[i] = blocks_len<EXTEND>(P, 2 * tid + i);
+    u32 bad = blocks_bad(P, n_free, all);
 #pragma unroll
     for (int i = 0; i < 2; i++) {
         const u32 r = 2 * tid + i;
         if (r >= P.n_req) continue;
-        change[i] = blocks_change<EXTEND>(P, r, c[i], c_new[i], bad);
-        s_c[r] = c[i];
-        s_at[r] = EXTEND ? (int)__ldcg(P.new_off + r) : c_new[i];
+        change[i] = blocks_change<EXTEND>(P, r, l[i], c_new[i], bad);
+        s_c[r] = l[i].c;
+        s_at[r] = (int)l[i].a;
     }
     long long total;
     const long long before = blocks_scan((long long)change[0] + change[1], s_scan, total);
     if (2 * tid < P.n_req) s_before[2 * tid] = (int)before;
     if (2 * tid + 1 < P.n_req) s_before[2 * tid + 1] = (int)(before + change[0]);
     const int status = blocks_status<EXTEND>(P, bad, n_free, total);
-    const u32 tokens = EXTEND && P.n_req ? (u32)__ldcg(P.new_off + P.n_req) : 0;
     if (ctas > 1) { cluster_arrive(); cluster_wait(); }                // the old state has been read
     if (cta == 0) {
 #pragma unroll
-        for (int i = 0; i < 2; i++) if (2 * tid + i < P.n_req) P.seq_out[2 * tid + i] = status ? c[i] : c_new[i];
+        for (int i = 0; i < 2; i++) if (2 * tid + i < P.n_req) P.seq_out[2 * tid + i] = status ? l[i].c : c_new[i];
         if (tid == 0) { *P.n_free_out = status ? n_free : EXTEND ? n_free - total : n_free + total; *P.status_out = status; }
     }
     if (status) return;
-    const u32 n = EXTEND ? tokens : (u32)total;
+    const u32 n = (u32)(EXTEND ? all : total);
     const int* at = EXTEND ? s_at : s_before;
     for (u32 i = cta * BLOCKS_THREADS + tid; i < n; i += ctas * BLOCKS_THREADS) {
         u32 lo = 0, hi = P.n_req - 1;                                  // the last request that begins at i or before
@@ -157,34 +165,40 @@ k_blocks_plan(const __grid_constant__ BlocksParams P) {
     cudaTriggerProgrammaticLaunchCompletion();
     const u32 tid = threadIdx.x;
     const long long n_free = __ldcg(P.n_free);
-    u32 bad = blocks_bad<EXTEND>(P, n_free);
+    u32 bad = blocks_bad(P, n_free, blocks_tokens<EXTEND>(P));
     long long carry = 0;
+    BlocksLen l[EACH] = {};
+    int32_t c_new[EACH] = {};
     for (unsigned long long r0 = 0; r0 < P.n_req; r0 += EACH * BLOCKS_THREADS) {
-        int32_t c[EACH], c_new;
         u32 change[EACH];
         long long mine = 0, total;
 #pragma unroll
+        for (int i = 0; i < EACH; i++) if (r0 + EACH * tid + i < P.n_req) l[i] = blocks_len<EXTEND>(P, (u32)(r0 + EACH * tid + i));
+#pragma unroll
         for (int i = 0; i < EACH; i++) {
             const unsigned long long r = r0 + EACH * tid + i;
-            c[i] = 0; change[i] = 0;
-            if (r < P.n_req) change[i] = blocks_change<EXTEND>(P, (u32)r, c[i], c_new, bad);
+            change[i] = r < P.n_req ? blocks_change<EXTEND>(P, (u32)r, l[i], c_new[i], bad) : 0;
             mine += change[i];
         }
         long long at = carry + blocks_scan(mine, s_scan, total);
 #pragma unroll
         for (int i = 0; i < EACH; i++) {
             const unsigned long long r = r0 + EACH * tid + i;
-            if (r < P.n_req) P.per[r] = make_int2(c[i], (int)(u32)at);
+            if (r < P.n_req) P.per[r] = make_int2(l[i].c, (int)(u32)at);
             at += change[i];
         }
         carry += total;
     }
     const int status = blocks_status<EXTEND>(P, bad, n_free, carry);
-    for (u32 r = tid; r < P.n_req; r += BLOCKS_THREADS) {              // (every length has been read: the new ones may lie over them)
-        const int32_t c = P.per[r].x;
-        int32_t c_new = c;
-        if (status == 0) c_new = EXTEND ? c + (int32_t)(__ldcg(P.new_off + r + 1) - __ldcg(P.new_off + r)) : __ldcg(P.keep + r);
-        P.seq_out[r] = c_new;
+    // every length has been read: the new ones may lie over them
+    if (P.n_req <= EACH * BLOCKS_THREADS) {
+#pragma unroll
+        for (int i = 0; i < EACH; i++) if (EACH * tid + i < P.n_req) P.seq_out[EACH * tid + i] = status ? l[i].c : c_new[i];
+    } else {
+        for (u32 r = tid; r < P.n_req; r += BLOCKS_THREADS) {
+            const int32_t c = P.per[r].x;
+            P.seq_out[r] = status ? c : EXTEND ? c + (int32_t)(__ldcg(P.new_off + r + 1) - __ldcg(P.new_off + r)) : __ldcg(P.keep + r);
+        }
     }
     if (tid == 0) {
         BlocksPlan q; q.n_free = n_free; q.total = carry; q.status = status; q.pad = 0;
