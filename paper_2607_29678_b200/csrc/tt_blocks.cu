@@ -25,9 +25,9 @@ static int blocks_args(BlocksParams& P, size_t n_req, const int32_t* seq_len, si
 }
 
 // `most`: entries (tokens, blocks) that the call may have to write.
-//   One kernel for up to BLOCKS_FEW requests and 4 tokens or 16 blocks a thread of the cluster: 64 requests of 500 tokens 7.4 us, as two kernels 9.0;
-//   1,000 of 60 12.5 and 10.3; 1,000 requests' 31,000 blocks back 7.0 and 11.0 (there are mostly fewer than fit in the list).
-//   Of one CTA up to an entry a thread: 256 and 1,000 requests of one token 4.1 and 4.9 us (a cluster 4.7 and 5.5), 64 of 64 6.9 (5.1).
+//   One kernel for up to BLOCKS_FEW requests and 4 tokens or 16 blocks a thread of the cluster: 64 requests of 500 tokens 6.6 us, as two kernels 8.2;
+//   1,000 of 60 11.8 and 9.3; 1,000 requests' 31,000 blocks back 6.6 and 9.7 (there are mostly fewer than fit in the list).
+//   Of one CTA up to an entry a thread: 256 and 1,000 requests of one token 3.3 and 4.2 us, of a cluster 3.9 and 4.8; 64 of 64 6.3 and 4.3.
 template <bool EXTEND>
 static int blocks_launch(const BlocksParams& P, size_t most, cudaStream_t st) {
     if (P.n_req <= BLOCKS_FEW && most <= (size_t)(EXTEND ? 4 : 16) * BLOCKS_CLUSTER * BLOCKS_THREADS) {

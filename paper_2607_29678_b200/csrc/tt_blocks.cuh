@@ -98,7 +98,7 @@ __device__ __forceinline__ int blocks_status(const BlocksParams& P, u32 bad, lon
 
 // Few requests: one kernel.  Every CTA of the cluster (one, or BLOCKS_CLUSTER of them) works out the whole plan in its shared memory, and they
 // wait for each other between the reading of the old state and the writing of the new one, which may lie in the same place.  256 requests of
-// one token 4.1 us, a chain of dependent loads.
+// one token 3.3 us, a chain of dependent loads.
 constexpr int BLOCKS_FEW = 2048, BLOCKS_CLUSTER = 8;
 template <bool EXTEND>
 __global__ void __launch_bounds__(BLOCKS_THREADS)
@@ -225,7 +225,7 @@ __device__ __forceinline__ u32 blocks_find(u32 lo, u32 hi, long long i, const F&
 // at a time.  The request of a tile is searched for only where it changes; of a tile with several requests their offsets and plans go to shared
 // memory, where every token looks for its own.  What all CTAs read is read by one warp of each: by every warp of the GPU it was a queue at one
 // slice of L2 (the blocks of 256 long requests back into the list 34 us).  Bound by the 16 bytes a token that it writes:
-// 22.7 million tokens of 256 requests 68 us behind a plan of 5, 5.3 TB/s.
+// 22.7 million tokens of 256 requests 68 us behind a plan of 4, 5.3 TB/s.
 constexpr int BLOCKS_WRITE_NT = 256, BLOCKS_WRITE_CTAS = 5, BLOCKS_TILE = 4 * BLOCKS_WRITE_NT, BLOCKS_STAGED = 1024;
 struct BlocksHead { long long n_free, total; int status; u32 r, last; };
 
