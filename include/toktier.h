@@ -207,8 +207,9 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
  *   grad_logprob   DEVICE float[n_rows].   grad_entropy, entropy  DEVICE float[n_rows], or both NULL (h = 0).
  *   grad_out       DEVICE, `dtype`, rows grad_stride entries apart: every row in use is written as a whole (n_vocab entries), the rows
  *                  behind the last document are left as they were.  It may be `logits` itself with the same stride; other overlaps are not allowed.
- * A row whose g and h are both 0 (g also where it is asked for nothing) gets zeros, and its logits are not read; so does a row whose lse is -inf.  A row whose lse is
- * NaN gets NaN.  status_out as above; the rest of the arguments too.
+ * A row whose g and h are both 0 (g also where it is asked for nothing) gets zeros, and its logits are not read; so does a row whose lse
+ * is below -2^60 (-inf, or a row of nothing but the type's lowest value).  A row whose lse is NaN gets NaN.  No p is above 1, and each is as exact as lse: off by
+ * some |lse| 2^-24 of itself.  status_out as above; the rest of the arguments too.
  * Both are asynchronous on `stream`, allocate nothing, need no workspace and may be captured into a graph.
  */
 enum { TT_BF16 = 0, TT_FP16 = 1, TT_FP32 = 2 };

@@ -572,16 +572,20 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
 // Reads a row once and writes it once; a CTA takes a stretch of SCORE_GRAD_NT * SCORE_U * rounds vectors of a row.  Bound by those bytes: 4,015 rows
 // of 200,000 bf16 logits 477 us, 6.7 TB/s (104 % of a copy's rate); in a long run of calls, at the power limit, 515.
 constexpr int SCORE_GRAD_NT = 256;
+constexpr float SCORE_NOTHING = -1.152921504606847e18f;        // -2^60: an lse below it says that all of the row is masked, by -inf or the type's lowest value
 
 struct ScoreGradRow { float scale, lse, A, B, hot; int32_t t; };
+__device__ __forceinline__ float score_not_above_0(float x) { float r; asm("min.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(x)); return r; }
 template <bool ENT>
 __device__ __forceinline__ void score_grad_pair(const ScoreGradRow& R, f32x2 x, float& a, float& b) {
-    const f32x2 l = pair_fma(x, pair_of(R.scale, R.scale), pair_of(-R.lse, -R.lse)), y = pair_mul(l, pair_of(1.44269504f, 1.44269504f));
-    float y0, y1, l0, l1;
-    pair_to(y, y0, y1);
+    float l0, l1;
+    pair_to(pair_fma(x, pair_of(R.scale, R.scale), pair_of(-R.lse, -R.lse)), l0, l1);
+    l0 = score_not_above_0(l0); l1 = score_not_above_0(l1);    // (an lse in the millions is off by more than 1 from rounding alone)
+    float y0, y1;
+    pair_to(pair_mul(pair_of(l0, l1), pair_of(1.44269504f, 1.44269504f)), y0, y1);
     const f32x2 p = pair_of(exp2_hw(y0), exp2_hw(y1));
     f32x2 f = pair_of(R.A, R.A);
-    if (ENT) { pair_to(l, l0, l1); f = pair_fma(pair_of(R.B, R.B), pair_of(fmaxf(l0, SCORE_LOW), fmaxf(l1, SCORE_LOW)), f); }
+    if (ENT) f = pair_fma(pair_of(R.B, R.B), pair_of(fmaxf(l0, SCORE_LOW), fmaxf(l1, SCORE_LOW)), f);
     pair_to(pair_mul(p, f), a, b);
 }
 template <bool ENT>
@@ -622,7 +626,7 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
     const float g = R.t < 0 ? 0.0f : __ldcg(P.g + row), h = ENT ? __ldcg(P.h + row) : 0.0f;
     R.lse = __ldcg(P.lse + row);
     R.scale = P.scale; R.A = -P.scale * (ENT ? fmaf(h, __ldcg(P.entropy + row), g) : g); R.B = -P.scale * h; R.hot = P.scale * g;
-    const bool zeros = (g == 0.0f && h == 0.0f) || R.lse == -INFINITY;
+    const bool zeros = (g == 0.0f && h == 0.0f) || R.lse < SCORE_NOTHING;
     // 16-byte vectors where rows of both lie alike in memory; else the logits are read entry by entry
     const u32 lead = min(P.n_vocab, (u32)((16 - ((uintptr_t)dx & 15)) & 15) / (u32)sizeof(T));
     const u32 n_vec = (P.n_vocab - lead) / N;

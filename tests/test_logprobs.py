@@ -114,9 +114,9 @@ def check_scores(logits, ids, bufs, ids_off=None, scale=1.0, untouched=None):
 def row_grad(x, scale, t, lse, ent, g, h):
     """(gradient, tolerance before the rounding to the output's type) of one row from its definition; lse and ent as handed to the kernel."""
     g = g if t >= 0 else 0.0
-    if (g == 0 and h == 0) or lse == -np.inf:
+    if (g == 0 and h == 0) or lse < -2.0 ** 60:
         return np.zeros_like(x), np.zeros_like(x)
-    lp = scale * x - lse
+    lp = np.minimum(scale * x - lse, 0.0)                                 # (what the rounding of lse leaves above 0)
     p = np.exp(lp)
     lpz = np.where(p > 0, lp, 0.0)
     hot = np.zeros_like(x)
@@ -125,7 +125,9 @@ def row_grad(x, scale, t, lse, ent, g, h):
     dx = scale * (g * (hot - p) - h * p * (lpz + ent))
     rel = 2.0 ** -22 + 4 * EPS * np.abs(lpz) + 4 * EPS                   # of p: the exponent's roundings and the hardware's exponential
     tol = scale * ((abs(g) + abs(h) * np.abs(lpz + ent)) * p * (rel + 6 * EPS) + 4 * EPS * abs(g) * hot + 3 * EPS * abs(h) * p * (np.abs(lpz) + abs(ent)))
-    return dx, tol + 2.0 ** -120                                           # (what is below the normal numbers of 32 bits may be 0)
+    # a probability below the normal numbers of 32 bits (2^-126) may be 0: an error of at most itself times its factor, whose logarithm is above -104
+    flushed = scale * 2.0 ** -126 * (abs(g) + abs(h) * (104 + abs(ent)))
+    return dx, tol + flushed
 
 
 def check_grad(logits, ids, bufs, g, h, grad, ids_off=None, scale=1.0, untouched=None):
@@ -391,7 +393,7 @@ def test_gradient_of_masked_and_broken_rows(tt, kind):
     x[0].masked_fill_(gone[0], -inf)
     x[1].masked_fill_(gone[1], low)
     x[2] = -inf
-    x[3] = low if kind == "fp16" else -5.0
+    x[3] = low                                                             # fp16: a uniform row; bf16 and fp32: nothing but masks, zeros
     x[4, 17] = float("nan")
     x[5, 17] = inf
     x[6, 17] = float("nan")
@@ -403,8 +405,33 @@ def test_gradient_of_masked_and_broken_rows(tt, kind):
     grad = torch.full_like(x, 5.0)
     tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=h)
     check_grad(x, ids, bufs, g, h, grad)
+    assert kind == "fp16" or bool((grad[3] == 0).all())
     assert bool((grad[2] == 0).all()) and bool((grad[6] == 0).all()) and bool(torch.isnan(grad[4:6].float()).all())
     assert bool((grad[0][gone[0]] == 0).sum() >= gone[0].sum() - 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradient_of_rows_far_from_0_stays_finite(tt, kind):
+    """Logits of a size at which lse is off by more than 1 from its rounding, and rows that the type's lowest value masks wholly, at several scales."""
+    import torch
+    low = torch.finfo(_kind(kind)).min
+    x = make_logits(kind, 6, 700, seed=8)
+    x[0] = low; x[0, ::3] = -float("inf")
+    x[1] = low
+    x[2] += 60_000.0 if kind == "fp16" else 3e8
+    x[3] -= 60_000.0 if kind == "fp16" else 3e8
+    x[4] = low; x[4, 5] = 0.25
+    ids = make_ids(6, 700, 1)
+    g, h = torch.ones(6, device="cuda"), torch.ones(6, device="cuda")
+    for scale in (1.0, 0.01, 1.5, 1e-6):
+        bufs, _ = run_scores(tt, x, ids, scale=scale)
+        for hh in (None, h):
+            grad = torch.full_like(x, 9.0)
+            tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=hh, scale=scale)
+            assert bool(torch.isfinite(grad).all()), scale
+            assert float(grad[4].float().abs().sum()) <= 2.0 * scale + 1e-3 or scale == 1e-6
+            check_grad(x[4:], ids[4:], {k: v[4:] for k, v in bufs.items() if k != "status"}, g[4:], None if hh is None else hh[4:], grad[4:], scale=scale)
 
 
 @pytest.mark.gpu
