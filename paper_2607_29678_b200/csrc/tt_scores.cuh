@@ -41,8 +41,13 @@ struct ScoreGradParams {
 __device__ __forceinline__ float score_f32(float x) { return x; }
 __device__ __forceinline__ float score_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float score_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-// A logit, past L1: a CTA may be placed while the kernel that wrote it still runs on the same SM.
-template <typename T> __device__ __forceinline__ float score_ld(const T* p) { return score_f32(__ldcg(p)); }
+// A logit, past L1: a CTA may be placed while the kernel that wrote it still runs on the same SM.  The 16-bit types are loaded as integers: the loads that
+// cuda_fp16.hpp and cuda_bf16.hpp define for them are assembly without `volatile`, which the compiler may take out of the condition it stands under
+// (entries behind the last row were read, and now and then lay behind the mapped memory).
+__device__ __forceinline__ float score_raw(const float* p) { return __ldcg(p); }
+__device__ __forceinline__ __half score_raw(const __half* p) { return __ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(p))); }
+__device__ __forceinline__ __nv_bfloat16 score_raw(const __nv_bfloat16* p) { return __ushort_as_bfloat16(__ldcg(reinterpret_cast<const unsigned short*>(p))); }
+template <typename T> __device__ __forceinline__ float score_ld(const T* p) { return score_f32(score_raw(p)); }
 __device__ __forceinline__ void score_put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void score_put(__half* p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void score_put(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
@@ -639,7 +644,7 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
         const T* e = x + lead + (size_t)v * N;
         uint4 r; T w[N];
 #pragma unroll
-        for (int i = 0; i < N; i++) w[i] = __ldcg(e + i);
+        for (int i = 0; i < N; i++) w[i] = score_raw(e + i);
         memcpy(&r, w, 16);
         return r;
     };
@@ -654,24 +659,24 @@ k_logprobs_grad(const __grid_constant__ ScoreGradParams P) {
         }
         __stcs(out + v, ScorePut<T>::vec(d));
     };
-    const u32 v1 = (u32)min((u64)n_vec, (u64)(part + 1) * share);
-    u64 v = (u64)part * share + tid;
+    const u32 v1 = min(n_vec, (part + 1) * share);             // (fewer than 2^29 vectors, a share of at most 2^12: no sum passes 32 bits)
+    u32 v = part * share + tid;
     if (zeros) {
         for (; v < v1; v += NT) __stcs(out + v, make_uint4(0, 0, 0, 0));
     } else {
         for (; v + (U - 1) * NT < v1; v += U * NT) {
             uint4 r[U];
 #pragma unroll
-            for (int i = 0; i < U; i++) r[i] = load((u32)v + i * NT);
+            for (int i = 0; i < U; i++) r[i] = load(v + i * NT);
 #pragma unroll
-            for (int i = 0; i < U; i++) put(r[i], (u32)v + i * NT);
+            for (int i = 0; i < U; i++) put(r[i], v + i * NT);
         }
         if (v < v1) {
             uint4 r[U];
 #pragma unroll
-            for (int i = 0; i < U; i++) if (v + i * NT < v1) r[i] = load((u32)v + i * NT);
+            for (int i = 0; i < U; i++) if (v + i * NT < v1) r[i] = load(v + i * NT);
 #pragma unroll
-            for (int i = 0; i < U; i++) if (v + i * NT < v1) put(r[i], (u32)v + i * NT);
+            for (int i = 0; i < U; i++) if (v + i * NT < v1) put(r[i], v + i * NT);
         }
     }
     const u32 loose = lead + (P.n_vocab - lead - n_vec * N);
