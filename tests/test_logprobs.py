@@ -692,3 +692,39 @@ def test_two_calls_at_once(tt):
         alone = torch.zeros_like(d)
         tt.logprobs_grad(v, ids, w, g, alone)
         assert torch.equal(alone, d)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_rows_at_the_end_of_the_memory(tt, kind):
+    """Logits whose last entry is the last one of a memory segment of its own, of sizes with entries on either side of the vectors."""
+    import torch
+    torch.cuda.empty_cache()
+    size = torch.finfo(_kind(kind)).bits // 8
+    whole = torch.zeros((32 << 20) // size, dtype=_kind(kind), device="cuda")      # (a segment is a multiple of 2 MB)
+    for rows, n, k in ((12, 23, 23), (1, 7, 1), (40, 1_001, 3), (3, 32_257, 20), (160, 5_003, 2), (500, 301, 5)):
+        x = whole[whole.numel() - rows * n:].view(rows, n)
+        x.copy_(torch.randn((rows, n), generator=torch.Generator(device="cuda").manual_seed(n), device="cuda"))
+        ids = make_ids(rows, n, n, none_every=5)
+        bufs, _ = run_scores(tt, x, ids, k)
+        check_scores(x, ids, bufs)
+        g = torch.randn(rows, device="cuda")
+        grad = torch.zeros((rows, n + 1), dtype=x.dtype, device="cuda")[:, :n]
+        tt.logprobs_grad(x, ids, bufs, g, grad)
+        check_grad(x, ids, bufs, g, None, grad)
+        want = grad.clone()
+        tt.logprobs_grad(x, ids, bufs, g, x)
+        assert torch.equal(x, want)
+
+
+def test_16_bit_logits_are_loaded_as_integers():
+    """The loads that cuda_fp16.hpp and cuda_bf16.hpp define past L1 (assembly without volatile) may be taken out of their conditions."""
+    import os
+    import re
+    src = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_29678_b200", "csrc", "tt_scores.cuh")
+    with open(src) as f:
+        text = f.read()
+    assert re.search(r"score_raw\(const __half\* p\) \{ return __ushort_as_half\(__ldcg\(reinterpret_cast<const unsigned short\*>\(p\)\)\); \}", text)
+    assert re.search(r"score_raw\(const __nv_bfloat16\* p\) \{ return __ushort_as_bfloat16\(__ldcg\(reinterpret_cast<const unsigned short\*>\(p\)\)\); \}", text)
+    for arg in re.findall(r"__ld[a-z]+\(([^()]*)", text):                  # of the others none takes the address of a logit: x, dx and e are such
+        assert not re.match(r"\s*(x|dx|e)\b", arg), arg
