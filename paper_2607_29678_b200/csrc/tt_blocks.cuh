@@ -3,7 +3,7 @@
 // With c_r tokens of request r in the cache and n_r new ones (release: c_r and the k_r that stay) the request's blocks change by
 //   ceil((c_r + n_r) / B) - ceil(c_r / B)      (release: ceil(c_r / B) - ceil(k_r / B)),
 // and an exclusive sum over the requests says which entries of the free list each of them gets (or fills).
-// What earlier kernels wrote is read past L1: a CTA may be placed while the kernel before it still runs on the same SM.
+// What earlier kernels wrote is read behind the wait for them (cudaGridDependencySynchronize), and past L1, since it is read once.
 // All lengths are read and the call decided on before anything of the new state is written, so that it may lie in the buffers of the old one.
 #pragma once
 #include "tt_host.cuh"
