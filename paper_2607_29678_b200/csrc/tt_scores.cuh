@@ -224,12 +224,15 @@ __device__ __forceinline__ u64 score_key(float x, u32 j) { return (u64)score_ord
 // that nothing is lost by it.  Where m c is too large for that (2^20: rho stays below 2^-4), M is a NaN and rho 0: the sums of such a batch are
 // NaNs, and it is worked out again as y = (x - m) c - rho, as are batches with a y of -inf (masked logits), whose product with 2^y is a NaN.
 // m starts at the lowest number, so that rows of -inf leave s = 0 and no difference of infinities arises.
+// A difference (x - m) c is (x / 2 - m / 2) 2 c: x - m may pass 32 bits where its product with a small c does not; both halves (but for
+// subnormal numbers, whose distances count at no scale) and 2 c are exact.
 struct ScoreSum { float m, s, u; };
 constexpr float SCORE_NONE = -3.402823466e38f, SCORE_LARGE = 1048576.0f;
 __device__ __forceinline__ float score_ref(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? M : NAN; }
 __device__ __forceinline__ float score_rho(float m, float c) { const float M = m * c; return fabsf(M) < SCORE_LARGE ? -fmaf(m, c, -M) : 0.0f; }
+__device__ __forceinline__ float score_half(float x, float m) { return fmaf(x, 0.5f, -0.5f * m); }
 __device__ __forceinline__ void score_raise(ScoreSum& a, float m, float c) {      // to a reference m >= a.m
-    const float y = fmaf(a.m - m, c, score_rho(a.m, c) - score_rho(m, c)), f = exp2_hw(y);
+    const float y = fmaf(score_half(a.m, m), 2.0f * c, score_rho(a.m, c) - score_rho(m, c)), f = exp2_hw(y);
     a.u = f * fmaf(fmaxf(y, SCORE_LOW2), a.s, a.u);
     a.s *= f;
     a.m = m;
@@ -240,7 +243,7 @@ template <typename V>
 __device__ __forceinline__ void score_add(const uint4& r, float m, float c, float rho, float& s, float& u) {
 #pragma unroll
     for (int e = 0; e < V::N; e++) {
-        const float y = fmaf(V::at(r, e) - m, c, -rho), w = exp2_hw(y);
+        const float y = fmaf(score_half(V::at(r, e), m), 2.0f * c, -rho), w = exp2_hw(y);
         s += w;
         u = fmaf(w, fmaxf(y, SCORE_LOW2), u);
     }
@@ -375,7 +378,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         if (bm > a.m) { score_raise(a, bm, c); ref = score_ref(bm, c); }
         // Once a thread has met masked logits a low number stands for -inf, whose terms are 0 without a NaN: where the largest logit is far above it, so
         // that its terms are 0, too, and the id's is above it, so that the count below is the same.
-        if (masked && (V::LOW - a.m) * c < SCORE_LOW && xt > V::LOW) {
+        if (masked && score_half(V::LOW, a.m) * (2.0f * c) < SCORE_LOW && xt > V::LOW) {
 #pragma unroll
             for (int i = 0; i < U; i++) r[i] = V::raised(r[i]);
         }
@@ -437,7 +440,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
         const u32 j = (u32)tid < lead ? tid : n_vec * N + tid;
         const float e = score_ld(x + j);
         if (e > a.m) score_raise(a, e, c);
-        const float y = fmaf(e - a.m, c, -score_rho(a.m, c)), w = exp2_hw(y);
+        const float y = fmaf(score_half(e, a.m), 2.0f * c, -score_rho(a.m, c)), w = exp2_hw(y);
         a.s += w;
         a.u = fmaf(w, fmaxf(y, SCORE_LOW2), a.u);
         if (RANK) n_before += e > xt || (e == xt && (int32_t)j < t);
@@ -559,7 +562,7 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
     const bool bad = sum.s != sum.s, nothing = sum.s == 0.0f;
     const float ln = logf(sum.s), ls = fmaf(score_rho(sum.m, c), 0.6931471806f, ln);       // ls: relative to m itself
     // (what rounding leaves of a probability of 1 is not above it, and no entropy is below 0)
-    const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : fminf(P.scale * (e - sum.m) - ls, 0.0f); };
+    const auto log_p = [&](float e) { return bad ? sum.s : nothing ? -INFINITY : fminf(fmaf(score_half(e, sum.m), 2.0f * P.scale, -ls), 0.0f); };
     if (tid == 0) {
         P.logprob[row] = t < 0 ? 0.0f : log_p(xt);
         if (P.lse) P.lse[row] = bad ? sum.s : nothing ? -INFINITY : fmaf(P.scale, sum.m, ls);

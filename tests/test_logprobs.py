@@ -728,3 +728,28 @@ def test_16_bit_logits_are_loaded_as_integers():
     assert re.search(r"score_raw\(const __nv_bfloat16\* p\) \{ return __ushort_as_bfloat16\(__ldcg\(reinterpret_cast<const unsigned short\*>\(p\)\)\); \}", text)
     for arg in re.findall(r"__ld[a-z]+\(([^()]*)", text):                  # of the others none takes the address of a logit: x, dx and e are such
         assert not re.match(r"\s*(x|dx|e)\b", arg), arg
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2, 700, 20_001, 150_000])
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_logits_over_the_whole_range_of_the_type(tt, kind, n):
+    """Distances between the logits of a row that pass 32 bits, at scales that make all of them count."""
+    import torch
+    top = torch.finfo(_kind(kind)).max
+    g = torch.Generator(device="cuda").manual_seed(n)
+    rows = 12
+    x = (torch.randn((rows, n), generator=g, device="cuda").double() * 1.7e38).clamp(-top, top).to(_kind(kind))
+    gone = torch.rand((rows, n), generator=g, device="cuda")
+    x[1] = torch.where(gone[1] < 0.5, torch.tensor(top, dtype=x.dtype, device="cuda"), torch.tensor(-top, dtype=x.dtype, device="cuda"))
+    x[2] = -top; x[2, n // 2:] = top
+    x[3] = -top; x[3, n - 1] = top
+    x[4:8].masked_fill_(gone[4:8] < 0.4, -float("inf"))
+    x[4:8, 0] = top
+    x[8] = torch.where(gone[8] < 0.5, torch.tensor(-float("inf"), device="cuda"), -gone[8] * 1e38).to(x.dtype); x[8, n - 1] = top
+    ids = make_ids(rows, n, n)
+    ids[:4] = n - 1
+    ids[4:8] = 0
+    for scale in (1.2e-38, 2e-38, 1e-37):
+        bufs, _ = run_scores(tt, x, ids, min(n, 5), scale=scale)
+        check_scores(x, ids, bufs, scale=scale)
