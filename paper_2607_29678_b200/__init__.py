@@ -413,6 +413,21 @@ def _logits(t, name="logits"):
     return kind, rows, n, max(step, n) if rows <= 1 else step
 
 
+def _documents(ids_off, n_docs, index):
+    """(address, number of documents) of offsets that may have room for more documents than there are."""
+    import torch
+    if ids_off is None:
+        if n_docs is not None:
+            raise ValueError("n_docs: there are no ids_off")
+        return None, 0
+    room = ids_off.numel() - 1
+    if n_docs is None:
+        n_docs = room
+    if not 0 <= n_docs <= room:
+        raise ValueError(f"n_docs: {n_docs} documents, ids_off has room for {room}")
+    return _dev(ids_off, torch.int64, "ids_off", None, index), n_docs
+
+
 def alloc_logprobs(n_rows: int, top_k: int = 0, device="cuda") -> dict:
     """Device buffers for logprobs(): dict(logprob, lse, entropy, rank, status and, with top_k, top_ids, top_logprobs), zeroed."""
     import torch
@@ -425,10 +440,11 @@ def alloc_logprobs(n_rows: int, top_k: int = 0, device="cuda") -> dict:
     return out
 
 
-def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None):
+def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None, n_docs: int | None = None):
     """tt_logprobs: logits = bfloat16 / float16 / float32 CUDA tensor [n_rows, n_vocab] (rows may lie apart), ids = int32 CUDA tensor
-    [n_rows], ids_off = int64 CUDA tensor [n_docs + 1] (as encode_batch leaves it) or None.  Results land in bufs as alloc_logprobs makes them; 'logprob'
-    and 'status' have to be there, the others are left out where they are missing; the second size of 'top_ids' is top_k."""
+    [n_rows], ids_off = int64 CUDA tensor [n_docs + 1] (as encode_batch leaves it) or None.  Where ids_off has room for more documents than the
+    batch had (Vocab.alloc's max_docs), n_docs says how many there are: what lies behind their offsets is an earlier batch's.  Results land in bufs as
+    alloc_logprobs makes them; 'logprob' and 'status' have to be there, the others are left out where they are missing; the second size of 'top_ids' is top_k."""
     import torch
     i32, f32 = torch.int32, torch.float32
     kind, rows, n, step = _logits(logits)
@@ -439,14 +455,14 @@ def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None):
     k = 0 if top is None else top.shape[1]
     _call("tt_logprobs", dev, stream,
           (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, i32, "ids", rows, dev),
-           None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1, k),
+           *_documents(ids_off, n_docs, dev), k),
           (_dev(bufs["logprob"], f32, "logprob", rows, dev), _opt(bufs, "lse", f32, rows, dev), _opt(bufs, "entropy", f32, rows, dev),
            _opt(bufs, "rank", i32, rows, dev), _dev(top, i32, "top_ids", rows * k, dev) if k else None,
            _dev(bufs["top_logprobs"], f32, "top_logprobs", rows * k, dev) if k else None, _dev(bufs["status"], i32, "status", 1, dev)))
 
 
-def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entropy=None, scale: float = 1.0, stream=None):
-    """tt_logprobs_grad: bufs as logprobs() left them for the same logits, ids, ids_off and scale ('lse', with grad_entropy also 'entropy';
+def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entropy=None, scale: float = 1.0, stream=None, n_docs: int | None = None):
+    """tt_logprobs_grad: bufs as logprobs() left them for the same logits, ids, ids_off, n_docs and scale ('lse', with grad_entropy also 'entropy';
     'status' is written again).  grad_logprob / grad_entropy: float32 CUDA tensors [n_rows]; grad: like logits, or logits itself."""
     import torch
     f32 = torch.float32
@@ -457,7 +473,7 @@ def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entr
         raise ValueError("grad: of the type, size and device of logits")
     _call("tt_logprobs_grad", dev, stream,
           (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
-           None if ids_off is None else _dev(ids_off, torch.int64, "ids_off", None, dev), 0 if ids_off is None else ids_off.numel() - 1,
+           *_documents(ids_off, n_docs, dev),
            _dev(bufs["lse"], f32, "lse", rows, dev), None if grad_entropy is None else _dev(bufs["entropy"], f32, "entropy", rows, dev),
            _dev(grad_logprob, f32, "grad_logprob", rows, dev), None if grad_entropy is None else _dev(grad_entropy, f32, "grad_entropy", rows, dev)),
           (grad.data_ptr(), gstep, _dev(bufs["status"], torch.int32, "status", 1, dev)))
@@ -497,8 +513,8 @@ def _blocks(state, bufs, block_size):
 
 
 def blocks_extend(new_off, state, block_size: int, bufs, stream=None):
-    """tt_blocks_extend: new_off = int64 CUDA tensor [n_req + 1] (encode_batch's ids_off, or a decode step's).  state: dict(seq_len, block_table,
-    free_blocks, n_free); bufs: dict(slots, seq_len, n_free, status, workspace and, if wanted, positions, requests), see alloc_blocks."""
+    """tt_blocks_extend: new_off = int64 CUDA tensor [n_req + 1] (the first n_req + 1 entries of encode_batch's ids_off, or a decode step's).
+    state: dict(seq_len, block_table, free_blocks, n_free); bufs: dict(slots, seq_len, n_free, status, workspace and, if wanted, positions, requests), see alloc_blocks."""
     import torch
     dev, n, before, behind = _blocks(state, bufs, block_size)
     slots = bufs["slots"]

@@ -99,3 +99,42 @@ def test_conversation_keeps_what_an_append_kept():
         blocks = -(-ids.size // BLOCK)
         assert np.array_equal(state["block_table"].cpu().numpy()[0, :blocks], pool.table[0, :blocks]) and len(set(pool.table[0, :blocks])) == blocks
         old_ids, old_off = ids, off
+
+
+def test_a_smaller_batch_in_the_buffers_of_a_larger_one():
+    """ids_off has room for more documents than the batch has: its end is the earlier batch's, and may ascend."""
+    import torch
+    import paper_2607_29678_b200 as tt
+    cfg = wl.CONFIGS["C1"]
+    v, cv = gpu_vocab("C1"), cpu_vocab("C1")
+    docs, doc_off = _documents([300, 200, 150, 700, 90, 260], 31)
+    bufs = v.alloc(int(doc_off[-1]), max_docs=len(docs))
+    v.encode_batch(to_dev(np.concatenate(docs)), torch.from_numpy(doc_off).cuda(), bufs)
+    torch.cuda.synchronize()
+    cap = int(bufs["ids_off"][-1])
+    few, few_off = _documents([120, 60], 71)
+    v.encode_batch(to_dev(np.concatenate(few)), torch.from_numpy(few_off).cuda(), bufs)
+    torch.cuda.synchronize()
+    off = bufs["ids_off"].cpu().numpy()
+    want = [cv.encode(d, cfg.pattern_id)[0] for d in few]
+    assert np.array_equal(off[:3], np.r_[0, np.cumsum([w.size for w in want])]) and (np.diff(off) >= 0).all() and off[-1] == cap > off[2]
+    n_vocab = 256 + cfg.n_merges
+    ids = bufs["ids"][:cap].clamp(0, n_vocab - 1)
+    logits = torch.randn((cap, n_vocab), generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    scores = tt.alloc_logprobs(cap, 2)
+    before = {k: np.zeros_like(t.cpu().numpy()) for k, t in scores.items()}
+    tt.logprobs(logits, ids, scores, ids_off=bufs["ids_off"], n_docs=2)
+    g, grad = torch.randn(cap, device="cuda"), torch.full_like(logits, 3.0)
+    tt.logprobs_grad(logits, ids, scores, g, grad, ids_off=bufs["ids_off"], n_docs=2)
+    torch.cuda.synchronize()
+    assert int(scores["status"]) == 0
+    check_scores(logits, ids, scores, ids_off=bufs["ids_off"][:3], untouched=before)
+    check_grad(logits, ids, scores, g, None, grad, ids_off=bufs["ids_off"][:3], untouched=np.full(tuple(grad.shape), 3.0))
+    tt.logprobs(logits, ids, scores, ids_off=bufs["ids_off"], n_docs=0)
+    torch.cuda.synchronize()
+    assert int(scores["status"]) == 0
+    for off_, n in ((bufs["ids_off"], 7), (bufs["ids_off"], -1), (None, 0)):
+        with pytest.raises(ValueError):
+            tt.logprobs(logits, ids, scores, ids_off=off_, n_docs=n)
+        with pytest.raises(ValueError):
+            tt.logprobs_grad(logits, ids, scores, g, grad, ids_off=off_, n_docs=n)
