@@ -753,3 +753,120 @@ def test_logits_over_the_whole_range_of_the_type(tt, kind, n):
     for scale in (1.2e-38, 2e-38, 1e-37):
         bufs, _ = run_scores(tt, x, ids, min(n, 5), scale=scale)
         check_scores(x, ids, bufs, scale=scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind,rows,n", [("fp32", 800, 33_001), ("fp16", 1_000, 57_345), ("bf16", 1_500, 33_001), ("bf16", 1_000, 100_257)])
+def test_gradient_of_many_long_rows(tt, kind, rows, n):
+    """A CTA takes several batches of a row: two of the first two sizes (5 and 4 CTAs a row), four of the others (2 and 4), on 148 SMs.  Every row equals,
+    bit by bit, that of a call on few rows (a batch a CTA); some rows, with their ids at the ends of the CTAs' stretches, against the definition."""
+    import torch
+    x = make_logits(kind, rows, n, seed=rows + n, pad=7, shift=1)
+    ids = make_ids(rows, n, n, none_every=9)
+    g, h = torch.randn(rows, device="cuda"), torch.randn(rows, device="cuda")
+    g[7::50] = 0.0; h[7::50] = 0.0
+    size = x.element_size()
+    whole = torch.full((rows, n + 7), 5.0, dtype=x.dtype, device="cuda")
+    odd = torch.full((rows, n + 12), 5.0, dtype=x.dtype, device="cuda")
+    grad = whole[:, :n]
+    vec, picked = 16 // size, [0, 7, rows - 1]
+    for i, batches in enumerate((1, 2, 4, 6, 8)):                          # the first and the last entry of stretches that end after so many batches
+        for k in (0, 1):
+            row = 11 + 2 * i + k
+            lead = (-(grad.data_ptr() + row * grad.stride(0) * size) % 16) // size
+            at = lead + batches * 4 * 256 * vec - k
+            if at < n:
+                ids[row] = at
+                picked.append(row)
+    ids[30], ids[31] = 0, n - 1
+    picked += [30, 31, rows // 2]
+    bufs, _ = run_scores(tt, x, ids)
+    some = torch.tensor(picked, device="cuda")
+    part = {k: v[some] for k, v in bufs.items() if k != "status"}
+    for hh in (None, h):
+        tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=hh)
+        check_grad(x[some], ids[some], part, g[some], None if hh is None else hh[some], grad[some])
+        for lo in range(0, rows, 100):
+            few = slice(lo, min(rows, lo + 100))
+            want = torch.empty_like(x[few])
+            tt.logprobs_grad(x[few], ids[few], {**{k: bufs[k][few] for k in ("lse", "entropy")}, "status": bufs["status"]}, g[few], want, grad_entropy=None if hh is None else hh[few])
+            assert torch.equal(grad[few], want), lo
+        tt.logprobs_grad(x, ids, bufs, g, odd[:, 3:n + 3], grad_entropy=hh)        # rows that do not lie as the logits' do
+        assert torch.equal(odd[:, 3:n + 3], grad)
+    assert bool((whole[:, n:] == 5.0).all()) and bool((odd[:, :3] == 5.0).all()) and bool((odd[:, n + 3:] == 5.0).all())
+    tt.logprobs_grad(x, ids, bufs, g, x, grad_entropy=h)                    # in place of the logits
+    assert torch.equal(x, grad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("rows,n,k", [(6, 1, 0), (6, 37, 3), (8, 4_353, 0), (6, 200_001, 20), (6, 200_001, 0), (300, 32_257, 1), (700, 70_001, 0), (1_100, 66_000, 2), (2_500, 4_353, 0)])
+def test_every_entry_counts_once(tt, kind, rows, n, k):
+    """Rows of one value, 0, between masked entries: the sum is their number, exact in 32 bits, and lse and entropy are its logarithm, off by at most
+    one unit of the last place (logf), which is less than what one entry more or less changes: 2^-20 and 1 / 200,001 at most."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    for share in (0.0, 0.5, 0.97):
+        gone = torch.rand((rows, n), generator=g, device="cuda") < share
+        gone[:, n // 2] = False
+        x = torch.zeros((rows, n), dtype=_kind(kind), device="cuda").masked_fill_(gone, -float("inf"))
+        ids = torch.full((rows,), n // 2, dtype=torch.int32, device="cuda")
+        bufs, _ = run_scores(tt, x, ids, k)
+        want = torch.log((~gone).sum(1).double())
+        unit = torch.where(want > 0, torch.exp2(torch.floor(torch.log2(want.clamp(min=2.0 ** -60))) - 23), 0.0)
+        for name in ("lse", "entropy", "logprob"):
+            off = (bufs[name].double() * (-1 if name == "logprob" else 1) - want).abs()
+            assert bool((off <= unit).all()), (share, name, float(off.max()))
+        assert torch.equal(bufs["rank"].long(), 1 + (~gone[:, :n // 2]).sum(1))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradient_against_the_formula_from_the_logits_alone(tt, kind):
+    """Softmax, entropy and gradient in 64 bits; what the kernel is handed (lse and entropy in 32 bits) counts towards the tolerance: p is off by expm1 of what its
+    logarithm is off by.  Rows that the type's lowest value masks wholly are uniform, in bf16 and fp32 with a gradient of zeros (their lse, below -2^60,
+    says nothing of their number), in fp16 with that of a uniform row."""
+    import torch
+    n, low = 1_501, torch.finfo(_kind(kind)).min
+    x = make_logits(kind, 10, n, seed=4)
+    gone = torch.rand((10, n), generator=torch.Generator(device="cuda").manual_seed(6), device="cuda") < 0.6
+    x[1].masked_fill_(gone[1], -float("inf"))
+    x[2].masked_fill_(gone[2], low)
+    x[3] += 100.0
+    x[4] -= 3_000.0
+    x[5] = low
+    x[6] = low; x[6].masked_fill_(gone[6], -float("inf"))
+    ids = make_ids(10, n, 1)
+    g, h = torch.randn(10, device="cuda"), torch.randn(10, device="cuda")
+    half = torch.finfo(x.dtype).eps / 2
+    least = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 0.0}[x.dtype]
+    xs = x.double().cpu().numpy()
+    for scale in (1.0, 0.75):
+        bufs, _ = run_scores(tt, x, ids, scale=scale)
+        grad = torch.full_like(x, 9.0)
+        tt.logprobs_grad(x, ids, bufs, g, grad, grad_entropy=h, scale=scale)
+        got = grad.double().cpu().numpy()
+        for i in range(10):
+            t = int(ids[i])
+            z = scale * xs[i]
+            count = int((xs[i] == low).sum())
+            if i in (5, 6):
+                assert abs(float(bufs["entropy"][i]) - np.log(count)) <= 2.0 ** -20
+                if kind != "fp16":
+                    assert (got[i] == 0).all()
+                    continue
+            m = z.max()
+            lse = m + np.log(np.exp(z - m).sum())
+            p, L = np.exp(z - lse), np.where(np.isfinite(z), z - lse, 0.0)
+            ent = -(p[p > 0] * L[p > 0]).sum()
+            w = row_scores(xs[i], scale, t, 0)["tol"]
+            hot = np.zeros(n); hot[t] = 1.0
+            gi, hi = float(g[i]), float(h[i])
+            want = scale * (gi * (hot - p) - hi * p * (np.where(p > 0, L, 0.0) + ent))
+            L = np.where(p > 0, L, 0.0)
+            dL = w["lse"] + EPS * (2 * np.abs(L) + 2 * abs(lse))           # of ln p: the lse handed over, its own rounding, that of the multiply-add
+            rel = np.expm1(dL + 2.0 ** -22 + 4 * EPS * np.abs(L))           # of p: and the hardware's exponential of it
+            tol = scale * (abs(gi) * p * rel + abs(hi) * p * ((np.abs(L) + ent) * rel + (dL + w["entropy"] + EPS * ent) * (1 + rel)))
+            tol += scale * 8 * EPS * (abs(gi) * (p + hot) + abs(hi) * p * (np.abs(L) + ent)) * (1 + rel) + scale * 2.0 ** -126 * (abs(gi) + abs(hi) * (104 + ent))
+            off = np.abs(got[i] - want) - (tol + half * (np.abs(want) + tol) + least)
+            assert off.max() <= 0, (i, scale, int(off.argmax()), got[i][off.argmax()], want[off.argmax()], tol[off.argmax()])
