@@ -207,9 +207,10 @@ int tt_spans(const tt_vocab* v, const int32_t* ids, const int64_t* count, size_t
  *   grad_logprob   DEVICE float[n_rows].   grad_entropy, entropy  DEVICE float[n_rows], or both NULL (h = 0).
  *   grad_out       DEVICE, `dtype`, rows grad_stride entries apart: every row in use is written as a whole (n_vocab entries), the rows
  *                  behind the last document are left as they were.  It may be `logits` itself with the same stride; other overlaps are not allowed.
- * A row whose g and h are both 0 (g also where it is asked for nothing) gets zeros, and its logits are not read; so does a row whose lse
- * is below -2^60 (-inf, or a row of nothing but the type's lowest value).  A row whose lse is NaN gets NaN.  No p is above 1, and each is as exact as lse: off by
- * some |lse| 2^-24 of itself.  status_out as above; the rest of the arguments too.
+ * A row whose g and h are both 0 (g also where it is asked for nothing) gets zeros, and its logits are not read.  So does a row whose lse is
+ * below -2^60: such an lse (-inf, or rounded to 2^37) no longer tells the probabilities.  A row of nothing but the lowest value of bf16 or fp32 is one, at
+ * scales above 2^-67, although tt_logprobs finds it uniform; in fp16 its lse is about -65504 scale, and it gets the gradient of a uniform row.  A row
+ * whose lse is NaN gets NaN.  No p is above 1, and each is as exact as lse: off by some |lse| 2^-24 of itself.  status_out as above; the rest of the arguments too.
  * Both are asynchronous on `stream`, allocate nothing, need no workspace and may be captured into a graph.
  */
 enum { TT_BF16 = 0, TT_FP16 = 1, TT_FP32 = 2 };
@@ -246,7 +247,7 @@ int tt_logprobs_grad(const void* logits, int dtype, size_t n_rows, size_t n_voca
  *                (or 2^31 - 1 tokens), more tokens than slots_cap.  TT_ERR_ARG comes first.  In either case the table, the list and the maps stay as they
  *                were, and seq_len_out and n_free_out get the lengths and the number that there were.
  *   workspace    DEVICE scratch of tt_blocks_workspace_bytes(n_req), 256-byte aligned, for calls that do not overlap in time.
- * n_req < 2^24, block_size and table_width < 2^31, slots_cap < 2^31, free_cap < 2^31; n_req = 0 gives TT_OK and copies *n_free.  Asynchronous on `stream`,
+ * n_req < 2^24, block_size and table_width < 2^31, slots_cap < 2^31, free_cap < 2^31; n_req = 0: TT_OK if *n_free is in its range, and *n_free_out = *n_free.  Asynchronous on `stream`,
  * may be captured into a graph.
  */
 size_t tt_blocks_workspace_bytes(size_t n_req);

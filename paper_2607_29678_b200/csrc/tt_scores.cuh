@@ -2,7 +2,8 @@
 //
 // With m the row's largest logit, a the scale, d_j = a (x_j - m) <= 0:  s = sum exp d,  u = sum d exp d,
 //   lse = a m + ln s,   ln p_t = d_t - ln s,   entropy = ln s - u / s.
-// Nothing cancels: ln s >= 0 and -u / s >= 0.
+// ln s >= 0 and -u / s >= 0: nothing cancels.  The kernel takes its sums against m a / ln 2 rounded (see ScoreSum): each of the two is off by up to 2^-5, the
+// same for both, which drops out of the entropy but for some 2^-29 of rounding; a sure row's is made 0 where that left less.
 #pragma once
 #include "tt_host.cuh"
 #include <cuda_bf16.h>
@@ -578,9 +579,11 @@ k_logprobs(const __grid_constant__ ScoreParams P) {
 
 // The gradient: with L = scale x_j - lse,  dx_j = exp(L) (A + B L) + [j = t] scale g,  A = -scale (g + h entropy), B = -scale h.
 // Reads a row once and writes it once; a CTA takes a stretch of SCORE_GRAD_NT * SCORE_U * rounds vectors of a row.  Bound by those bytes: 4,015 rows
-// of 200,000 bf16 logits 477 us, 6.7 TB/s (104 % of a copy's rate); in a long run of calls, at the power limit, 515.
+// of 200,000 bf16 logits 477-489 us, 6.6-6.7 TB/s (a copy that reads and writes as much: 497); in a long run of calls, at the power limit, 515.
 constexpr int SCORE_GRAD_NT = 256;
-constexpr float SCORE_NOTHING = -1.152921504606847e18f;        // -2^60: an lse below it says that all of the row is masked, by -inf or the type's lowest value
+// -2^60: an lse below it, -inf or rounded to 2^37, does not tell a row's probabilities.  (A row of nothing but the lowest value has such a one in bf16 and fp32, but for scales
+// below 2^-67; in fp16 only at scales above 2^44.)
+constexpr float SCORE_NOTHING = -1.152921504606847e18f;
 
 struct ScoreGradRow { float scale, lse, A, B, hot; int32_t t; };
 __device__ __forceinline__ float score_not_above_0(float x) { float r; asm("min.NaN.f32 %0, %1, 0f00000000;" : "=f"(r) : "f"(x)); return r; }
