@@ -389,9 +389,14 @@ def _call(name, index, stream, before, behind):
     if stream is not None and stream.device.index != index:
         raise ValueError(f"stream of {stream.device}, tensors on cuda:{index}")
     f = getattr(_lib or lib(), name)
-    if index == torch._C._cuda_getDevice():
-        # (the address alone: torch.cuda.current_stream() makes an object for it, a microsecond of every call)
-        rc = f(*before, torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream, *behind)
+    if index == torch.cuda.current_device():
+        if stream is not None:
+            at = stream.cuda_stream
+        else:
+            # (the address alone, where torch has a call for it: torch.cuda.current_stream() makes an object, a microsecond of every call)
+            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+            at = torch.cuda.current_stream(index).cuda_stream if raw is None else raw(index)
+        rc = f(*before, at, *behind)
     else:
         with torch.cuda.device(index):
             rc = f(*before, _stream_ptr(stream), *behind)

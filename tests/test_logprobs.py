@@ -870,3 +870,21 @@ def test_gradient_against_the_formula_from_the_logits_alone(tt, kind):
             tol += scale * 8 * EPS * (abs(gi) * (p + hot) + abs(hi) * p * (np.abs(L) + ent)) * (1 + rel) + scale * 2.0 ** -126 * (abs(gi) + abs(hi) * (104 + ent))
             off = np.abs(got[i] - want) - (tol + half * (np.abs(want) + tol) + least)
             assert off.max() <= 0, (i, scale, int(off.argmax()), got[i][off.argmax()], want[off.argmax()], tol[off.argmax()])
+
+
+def test_streams_of_a_torch_without_the_private_call(tt, monkeypatch):
+    """The current stream's address, by the private call where there is one and by the public one where there is not; a stream of the caller's."""
+    import types
+    import torch
+    seen = []
+    monkeypatch.setattr(tt, "_lib", types.SimpleNamespace(tt_f=lambda *a: seen.append(a) or tt.TT_OK))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: types.SimpleNamespace(cuda_stream=100 + index))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 200 + index, raising=False)
+    tt._call("tt_f", 1, None, (7,), (8,))
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    tt._call("tt_f", 1, None, (7,), (8,))
+    tt._call("tt_f", 1, types.SimpleNamespace(cuda_stream=300, device=types.SimpleNamespace(index=1)), (7,), (8,))
+    assert seen == [(7, 201, 8), (7, 101, 8), (7, 300, 8)]
+    with pytest.raises(ValueError):
+        tt._call("tt_f", 1, types.SimpleNamespace(cuda_stream=300, device=types.SimpleNamespace(index=0)), (7,), (8,))
