@@ -389,14 +389,13 @@ def _call(name, index, stream, before, behind):
     if stream is not None and stream.device.index != index:
         raise ValueError(f"stream of {stream.device}, tensors on cuda:{index}")
     f = getattr(_lib or lib(), name)
-    if index == torch.cuda.current_device():
-        if stream is not None:
-            at = stream.cuda_stream
-        else:
-            # (the address alone, where torch has a call for it: torch.cuda.current_stream() makes an object, a microsecond of every call)
-            raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-            at = torch.cuda.current_stream(index).cuda_stream if raw is None else raw(index)
-        rc = f(*before, at, *behind)
+    try:
+        # (the address alone: torch.cuda.current_stream() makes an object for it, a microsecond of every call)
+        here, current = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    except AttributeError:                                                 # torch's own, and not in every version of it
+        here, current = torch.cuda.current_device, lambda i: torch.cuda.current_stream(i).cuda_stream
+    if index == here():
+        rc = f(*before, current(index) if stream is None else stream.cuda_stream, *behind)
     else:
         with torch.cuda.device(index):
             rc = f(*before, _stream_ptr(stream), *behind)
@@ -458,9 +457,9 @@ def logprobs(logits, ids, bufs, ids_off=None, scale: float = 1.0, stream=None, n
     if (top is None) != (bufs.get("top_logprobs") is None) or (top is not None and (top.dim() != 2 or top.shape[0] != rows)):
         raise ValueError("top_ids and top_logprobs: both [n_rows, top_k], or neither")
     k = 0 if top is None else top.shape[1]
+    off, docs = (None, 0) if ids_off is None and n_docs is None else _documents(ids_off, n_docs, dev)
     _call("tt_logprobs", dev, stream,
-          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, i32, "ids", rows, dev),
-           *_documents(ids_off, n_docs, dev), k),
+          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, i32, "ids", rows, dev), off, docs, k),
           (_dev(bufs["logprob"], f32, "logprob", rows, dev), _opt(bufs, "lse", f32, rows, dev), _opt(bufs, "entropy", f32, rows, dev),
            _opt(bufs, "rank", i32, rows, dev), _dev(top, i32, "top_ids", rows * k, dev) if k else None,
            _dev(bufs["top_logprobs"], f32, "top_logprobs", rows * k, dev) if k else None, _dev(bufs["status"], i32, "status", 1, dev)))
@@ -476,9 +475,9 @@ def logprobs_grad(logits, ids, bufs, grad_logprob, grad, ids_off=None, grad_entr
     gkind, grows, gn, gstep = _logits(grad, "grad")
     if gkind != kind or grows != rows or gn != n or grad.get_device() != dev:
         raise ValueError("grad: of the type, size and device of logits")
+    off, docs = (None, 0) if ids_off is None and n_docs is None else _documents(ids_off, n_docs, dev)
     _call("tt_logprobs_grad", dev, stream,
-          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev),
-           *_documents(ids_off, n_docs, dev),
+          (logits.data_ptr(), kind, rows, n, step, scale, _dev(ids, torch.int32, "ids", rows, dev), off, docs,
            _dev(bufs["lse"], f32, "lse", rows, dev), None if grad_entropy is None else _dev(bufs["entropy"], f32, "entropy", rows, dev),
            _dev(grad_logprob, f32, "grad_logprob", rows, dev), None if grad_entropy is None else _dev(grad_entropy, f32, "grad_entropy", rows, dev)),
           (grad.data_ptr(), gstep, _dev(bufs["status"], torch.int32, "status", 1, dev)))

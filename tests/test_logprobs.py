@@ -878,6 +878,7 @@ def test_streams_of_a_torch_without_the_private_call(tt, monkeypatch):
     import torch
     seen = []
     monkeypatch.setattr(tt, "_lib", types.SimpleNamespace(tt_f=lambda *a: seen.append(a) or tt.TT_OK))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda index=None: types.SimpleNamespace(cuda_stream=100 + index))
     monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 200 + index, raising=False)
