@@ -889,3 +889,30 @@ def test_streams_of_a_torch_without_the_private_call(tt, monkeypatch):
     assert seen == [(7, 201, 8), (7, 101, 8), (7, 300, 8)]
     with pytest.raises(ValueError):
         tt._call("tt_f", 1, types.SimpleNamespace(cuda_stream=300, device=types.SimpleNamespace(index=0)), (7,), (8,))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_a_row_of_as_many_entries_as_there_may_be(tt, kind):
+    """2^31 - 1 logits, all but a thousand of them masked: their places are told apart up to the last one, gradient included (in place)."""
+    import torch
+    n = 2**31 - 1
+    x = torch.full((1, n), -float("inf"), dtype=_kind(kind), device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(3)
+    at = torch.cat([torch.randint(0, n, (1_000,), generator=g, device="cuda"), torch.tensor([0, 1, 2**30 - 1, 2**30, n - 2, n - 1], device="cuda")]).unique()
+    x[0, at] = torch.randn(at.numel(), generator=g, device="cuda").to(x.dtype)
+    x[0, -1] = 6.0
+    small = x[0, at].double().cpu().numpy()
+    place = at.cpu().numpy()
+    for t in (0, 500, at.numel() - 1):
+        ids = torch.tensor([int(place[t])], dtype=torch.int32, device="cuda")
+        bufs, _ = run_scores(tt, x, ids, 32)
+        w = row_scores(small, 1.0, t, 32)
+        assert int(bufs["rank"]) == w["rank"] and np.array_equal(bufs["top_ids"][0].cpu().numpy(), place[w["top_ids"]])
+        for name in ("logprob", "lse", "entropy", "top_logprobs"):
+            assert near(bufs[name][0].cpu().numpy(), w[name], w["tol"][name]), name
+    one, h = torch.ones(1, device="cuda"), torch.full((1,), 0.5, device="cuda")
+    part = {k: v for k, v in bufs.items() if k != "status"}
+    tt.logprobs_grad(x, ids, bufs, one, x, grad_entropy=h)
+    assert int(x.count_nonzero()) <= at.numel()
+    check_grad(torch.from_numpy(small)[None], torch.tensor([t]), part, one, h, x[:, at])
