@@ -28,6 +28,8 @@ static int blocks_args(BlocksParams& P, size_t n_req, const int32_t* seq_len, si
 //   One kernel for up to BLOCKS_FEW requests and 4 tokens or 16 blocks a thread of the cluster: 64 requests of 500 tokens 6.6 us, as two kernels 8.2;
 //   1,000 of 60 11.8 and 9.3; 1,000 requests' 31,000 blocks back 6.6 and 9.7 (there are mostly fewer than fit in the list).
 //   Of one CTA up to an entry a thread: 256 and 1,000 requests of one token 3.3 and 4.2 us, of a cluster 3.9 and 4.8; 64 of 64 6.3 and 4.3.
+//   The room in the buffers decides, since the host does not know what there is to write: 256 requests of one token take 12.8 us (two kernels) where
+// `slots` has room for more than 32,768 tokens, and 1,000 14.5.  Maps of their own for decode steps have the small form.
 template <bool EXTEND>
 static int blocks_launch(const BlocksParams& P, size_t most, cudaStream_t st) {
     if (P.n_req <= BLOCKS_FEW && most <= (size_t)(EXTEND ? 4 : 16) * BLOCKS_CLUSTER * BLOCKS_THREADS) {

@@ -26,6 +26,8 @@ static cudaError_t launch_logprobs_nt(const ScoreParams& P, cudaStream_t st) {
 //   But between half a round and one and a half of CTAs of 128 threads, where the SMs get one or two more or less: long 16-bit rows, bound by arithmetic
 //   too, take 256 (1,024 rows of 400 KB: 64 threads 86 us, 128 85, 256 73; with alternatives 124, 100, 93), others behind a full round 64, all at
 //   once (1,000 rows of 400 KB in 32 bits: 66, 90, 74; 1,100 of 64 KB: 27, 28, 30).
+//   These borders lie between sizes that were measured, 8.7 and 64 KB for the first, 64 and 400 KB for the second, and some rows outside them would gain by another form: 2,200 of
+// 400 KB with alternatives 128 threads 189 us, 256 175; 600 without 256 threads 51.7, 128 in clusters of two 48.3.
 //   Fewer rows: a cluster for a row as long as its CTAs have places and 48 KB each (one row of 200 KB: 1 CTA 11.6 us, 4 7.7; 64 rows of 400 KB:
 //   1 CTA 21, 4 14.9, 8 24; 300 of 400 KB: 42, of 2 CTAs 36, 4 37, 8 46; 64 rows of 64 KB: 1 CTA 8.8, 2 9.2, 8 15.7).
 template <typename T>
